@@ -322,6 +322,34 @@ int32_t mkv_decode_attention_scored(mkv_pool* pool, const void* q_dev, const int
                                     int32_t max_pages, float scale, float* out_dev, float* lse_dev,
                                     float* page_mass_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
 
+/* Attention of the last tokens of every request over the paged cache that holds them and everything before: a prompt's
+ * chunk, draft tokens to be verified, or a batch that mixes chunks with single tokens.  Request b has seq_lens[b] cached
+ * tokens (Append comes first), of which the last n_b = q_starts[b + 1] - q_starts[b] are the chunk.  Row i of the chunk
+ * is position p = seq_lens[b] - n_b + i and sees the positions 0 .. p, pages in both formats under one softmax
+ * (Section 3.3, Section 4.1).
+ *   q            device, bf16 [n_rows][n_q_heads][d], q_stride elements from a token to the next (a multiple of 8, at
+ *                least n_q_heads * d: a slice of a fused projection is taken as it stands)
+ *   q_starts     device, int32 [B + 1]: first row of every request, ascending from 0 or more; n_b may be 0.  Rows behind
+ *                q_starts[B] and before q_starts[0] are neither read nor written.  Rows outside [0, n_rows) or a negative
+ *                n_b: the request is left out and the event recorded in the status word
+ *   block_table, tier_tag, seq_lens   as mkv_decode_attention (a length beyond the table's row is cut and recorded, an
+ *                invalid entry skipped and recorded; a Stale page that is not full is invalid)
+ *   scale        finite; may be 0 or negative
+ *   out          device, bf16 [n_rows][n_q_heads][d], dense.  A row that sees nothing (its position is negative, or all
+ *                its pages invalid) is 0 with lse = -inf
+ *   lse          device, fp32 [n_rows][n_q_heads], natural logarithm, or NULL
+ *   workspace    device, at least mkv_chunk_workspace_bytes(cfg, B, max_pages) bytes, 256-byte aligned, any contents; two
+ *                calls that overlap on the GPU need two buffers
+ * Keys, values and probabilities enter the tensor core as fp16 (FP8 pages exactly) and are summed in fp32: out is within
+ * a bf16 rounding and about 1e-3 of the exact result, lse within about 1e-3.  Values are held relative to a power of two near
+ * the pool's scales, so that whatever Demote writes fits.  NaN in a key or value reaches the rows that see it, and no
+ * others.  Three launches; results do not depend on what else runs.  No host synchronisation. */
+int32_t mkv_chunk_workspace_bytes(const mkv_pool_config* cfg, int32_t max_batch, int32_t max_pages, size_t* bytes);
+int32_t mkv_chunk_attention(mkv_pool* pool, const void* q_dev, int64_t q_stride, int32_t n_rows, const int32_t* q_starts_dev,
+                            const int32_t* block_table_dev, const uint8_t* tier_tag_dev, const int32_t* seq_lens_dev, int32_t B,
+                            int32_t max_pages, float scale, void* out_dev, float* lse_dev, void* workspace_dev,
+                            size_t workspace_bytes, void* stream);
+
 /* Eq. (attention-score): r_p = mean over the sampled head set of q~_{h,p}, a_p <- beta a_p + (1-beta) r_p
  * for every page below each request's length (others untouched).
  *   page_mass    device, fp32 [B][n_q_heads][max_pages] from mkv_decode_attention_scored

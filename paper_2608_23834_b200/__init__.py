@@ -36,6 +36,7 @@ EXPORTS = [
     "mkv_decode_attention_static", "mkv_promote", "mkv_seq_promote",
     "mkv_decode_attention_scored", "mkv_page_score_update", "mkv_page_score_update_paged",
     "mkv_decode_attention_layers", "mkv_append_layers", "mkv_pool_set_wait_limit_ns", "mkv_seq_release",
+    "mkv_chunk_workspace_bytes", "mkv_chunk_attention",
 ]
 MAX_LAYERS_PER_CALL = 32
 
@@ -110,6 +111,9 @@ def lib():
             "mkv_decode_attention_layers": [C.POINTER(LayerCall), C.c_int32, vp, C.c_int32, C.c_int32, C.c_float,
                                             C.c_size_t, vp],
             "mkv_append_layers": [C.POINTER(LayerAppend), C.c_int32, vp, C.c_int32, vp],
+            "mkv_chunk_workspace_bytes": [cfgp, C.c_int32, C.c_int32, szp],
+            "mkv_chunk_attention": [vp, vp, C.c_int64, C.c_int32, vp, vp, vp, vp, C.c_int32, C.c_int32, C.c_float, vp, f32p,
+                                    vp, C.c_size_t, vp],
             "mkv_pool_set_wait_limit_ns": [vp, C.c_uint64],
             "mkv_seq_create": [vp, C.POINTER(vp)],
             "mkv_seq_finish": [vp],
@@ -211,7 +215,7 @@ class Pool:
             _check(L.mkv_pool_create(C.byref(self.cfg), _ptr(self.fp8_arena), _ptr(self.tq3_arena), _stream(None),
                                      C.byref(h)), "mkv_pool_create")
             self.handle = h
-            self._ref = native().pool_ref(h.value, n_kv_heads, n_q_heads, head_dim)     # what the native calls need of the pool
+            self._ref = native().pool_ref(h.value, n_kv_heads, n_q_heads, head_dim, self.fp8_arena.device.index)   # what the native calls need
             _check(L.mkv_workspace_init(_ptr(self.workspace), self.ws_bytes, _stream(None)), "mkv_workspace_init")
 
     def close(self):
@@ -349,6 +353,49 @@ class Pool:
                                                  _ptr(page_mass), _ptr(ws), ws.numel(), _stream(stream)),
                "mkv_decode_attention_scored")
         return out, lse, page_mass
+
+    # ---- chunks of new tokens
+    def chunk_workspace(self, max_batch: int, max_pages: int) -> torch.Tensor:
+        """Workspace of chunk_attention for up to max_batch requests of up to max_pages pages.  A program keeps one per
+        stream (calls that overlap on the GPU, captured ones among them, need one each)."""
+        n = C.c_size_t()
+        _check(lib().mkv_chunk_workspace_bytes(C.byref(self.cfg), max_batch, max_pages, C.byref(n)), "mkv_chunk_workspace_bytes")
+        return torch.empty(n.value, dtype=torch.uint8, device=self.device)
+
+    def chunk_attention(self, q, q_starts, block_table, tier_tag, seq_lens, scale, out=None, lse=None, workspace=None, stream=None):
+        """mkv_chunk_attention: attention of the last q_starts[b + 1] - q_starts[b] of the seq_lens[b] cached tokens of every
+        request over its pages.  q: bf16 [rows][hq][d], the rows may lie apart (a slice of a fused projection); returns
+        bf16 [rows][hq][d].  Rows that no request has are left as they are in a given `out` and are 0 in a new one."""
+        if out is not None and _native_rc(_native.chunk_attention(self._ref, q, q_starts, block_table, tier_tag, seq_lens, scale,
+                                                                  out, lse, workspace, stream), "mkv_chunk_attention"):
+            return out
+        B, n = seq_lens.numel(), q.shape[0]
+        self._check_rows(q, n, self.hq, "q")
+        assert q_starts.dtype == torch.int32 and q_starts.is_contiguous() and q_starts.numel() == B + 1
+        assert block_table.dtype == torch.int32 and block_table.is_contiguous() and block_table.dim() == 2 and block_table.shape[0] == B
+        assert tier_tag.dtype == torch.uint8 and tier_tag.is_contiguous() and tier_tag.shape == block_table.shape
+        assert seq_lens.dtype == torch.int32 and seq_lens.is_contiguous()
+        if out is None:
+            out = torch.zeros((n, self.hq, self.d), dtype=torch.bfloat16, device=q.device)
+        assert out.dtype == torch.bfloat16 and out.is_contiguous() and out.shape == q.shape
+        if lse is not None:
+            assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2]
+        if workspace is None:
+            workspace = self.chunk_workspace(max(B, 1), max(block_table.shape[1], 1))
+        assert workspace.dtype == torch.uint8 and workspace.is_contiguous()
+        tensors = [q, q_starts, block_table, tier_tag, seq_lens, out, workspace] + ([lse] if lse is not None else [])
+        assert all(t.device == self.fp8_arena.device for t in tensors), "every tensor is on the pool's device"
+        with torch.cuda.device(self.fp8_arena.device):
+            _check(lib().mkv_chunk_attention(self.handle, _ptr(q), q.stride(0), n, _ptr(q_starts), _ptr(block_table), _ptr(tier_tag),
+                                             _ptr(seq_lens), B, block_table.shape[1], float(scale), _ptr(out), _ptr(lse),
+                                             _ptr(workspace), workspace.numel(), _stream(stream)), "mkv_chunk_attention")
+        return out
+
+    def _check_rows(self, x, n, heads, name):
+        """bf16 [n][heads][d] whose tokens may lie apart: heads and dims dense, tokens a multiple of 16 bytes apart."""
+        assert x.dtype == torch.bfloat16 and x.shape == (n, heads, self.d), f"{name}: bf16 [{n}][{heads}][{self.d}]"
+        assert x.stride(2) == 1 and (heads == 1 or x.stride(1) == self.d), f"{name}: dense heads"
+        assert n <= 1 or (x.stride(0) % 8 == 0 and x.stride(0) >= heads * self.d), f"{name}: token stride"
 
 
 def decode_attention_layers(pools, qs, block_tables, tier_tags, seq_lens, scale, outs, lses=None, stream=None):

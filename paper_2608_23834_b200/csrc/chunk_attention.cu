@@ -1,0 +1,1254 @@
+// Attention of a chunk of new tokens over the mixed-format paged cache (mkv_chunk_attention).
+//
+// Row i of request b is its position p = seq_lens[b] - n_b + i (n_b new tokens, cached already).  For every query head
+//   s_t = scale q . k_t for t <= p,   out = sum_t exp(s_t) v_t / sum_t exp(s_t),
+// over the FP8 and Stale pages of the request's table row under one softmax (Section 3.3), each page read in its own
+// format (Section 4.1).  Stale keys stay in the rotated domain: s_t = scale q' . c_t g_t with q' = d^-1/2 H (sigma . q).
+//
+// Mapping to the hardware
+//   * The rows of a tile are (token, query head) pairs of one KV head, 128 per tensor-memory accumulator: a query group
+//     shares every unpacked key and value.  A block takes two such row tiles at d = 128 and one at d = 256 (the output
+//     accumulators, 256 columns, and two score buffers of 128 columns fill tensor memory) and walks tiles of 128 keys.
+//   * Each key tile holds pages of one format (chunk_plan_kernel sorts a row's pages by format), so that the products
+//     take one query: the rotated one for Stale tiles, then the plain one, written over it, for FP8 tiles.
+//   * Pages are unpacked once per block to fp16 in shared memory, K-major with the 128-byte swizzle, by eight warps
+//     (e4m3 -> fp16 is exact; Stale keys are level * g, values code * scale + zero, each rounded to fp16: 2^-12 of an
+//     element on average, as the probabilities' rounding and far below the output's bf16).  A lane of the packed
+//     fragment order holds scattered dims (keys) and tokens (values): the order of the contraction is free, so query dims
+//     and key rows are permuted such that every lane's share is one 16-byte store without bank conflicts.
+//   * One thread issues the products S = Q K^T (both operands in shared memory) and O += P V (P in tensor memory, over
+//     the scores it came from), the scores of the tile after next before the softmax of this one has finished.
+//   * A softmax thread owns a row (its tensor-memory lane): no exchange between threads.  The reference of the
+//     exponentials is raised only when a score exceeds it by 2^15, which keeps P within fp16 and rescaling of O rare;
+//     it lies 7 below the maximum, so that probabilities down to 2^-31 of the largest are not flushed.
+//   * (unit, key tiles) pairs are cut evenly over the SMs; a unit that several blocks share leaves fp32 partials
+//     (m, l, O) in the workspace and chunk_merge_kernel joins them (Eq. softmax-merge), in the order of the blocks.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math_constants.h>
+
+#include "mkv_internal.cuh"
+#include "tensor_ptx.cuh"
+
+namespace mkv {
+namespace chunk {
+
+constexpr int kMaxBlocks = 160;              // of the scan's grid: sizes the partials
+constexpr int kKeys = 128;                   // keys of a tile: eight runs of 16 tokens
+constexpr int kUnitCost = 2;                 // what a unit costs besides its key tiles (query, epilogue), in key tiles
+constexpr int kLeastShare = 3;               // key tiles of a block at least
+constexpr float kShift = 7.f, kSlack = 8.f;  // see above: probabilities are at most 2^(kShift + kSlack)
+constexpr int kNoPos = 0x7fffffff;
+
+// What chunk_plan_kernel leaves of a request.  Runs are of 16 tokens.
+struct Request {
+    int n_new, row0, len;
+    int n_stale, n_fp8;          // runs in the two lists
+    int stale_end;               // runs of the row up to the last Stale page
+    int exact;                   // every page of the row is in a list
+    int pad;
+    long long cost;              // of one KV head: the units' key tiles + kUnitCost each
+};
+struct Merge {
+    int b, h, rt, last;          // unit, last block that has a part of it; b < 0: nothing to merge
+    int first_slot, pad[3];
+};
+
+struct Params {
+    const uint8_t *fp8, *tq3;
+    int fp8_pages, tq3_pages, hkv, group, tiles;
+    SigmaBits sigma;
+    float sc2;                   // |scale| log2 e
+    int negative;                // scale < 0: the queries change their sign
+    float k_scale, v_scale;      // of FP8 pages
+    int ke, ve;                  // exponents of the units 2^ke, 2^ve in which Stale keys and values are held as fp16
+    const __nv_bfloat16* q;
+    long long q_stride;          // elements from a token to the next
+    int n_rows;
+    const int32_t *starts, *bt, *lens;
+    const uint8_t* tags;
+    int B, max_pages;
+    __nv_bfloat16* out;
+    float* lse;
+    Request* req;
+    int2* list;                  // [B][max_pages] (logical page, id): Stale pages from the front, FP8 pages from the back
+    float* part_o;               // [2 * blocks][rows][D]
+    float2* part_ml;             // [2 * blocks][rows] (reference, sum)
+    Merge* merge;
+    uint32_t* status;
+    unsigned long long wait_ns;
+};
+
+template <int D>
+struct Geo {
+    static constexpr int NT = D == 128 ? 2 : 1;                 // row tiles of a block
+    static constexpr int ROWS = 128 * NT;
+    static constexpr int STAGES = D == 128 ? 2 : 1;             // key tiles, and value tiles, in shared memory
+    static constexpr int Q_TILE = 128 * D * 2, K_TILE = kKeys * D * 2, V_TILE = K_TILE;
+    static constexpr int SOFT_WARPS = 4 * NT, UNPACK_WARPS = 8;
+    static constexpr int MMA_WARP = SOFT_WARPS + UNPACK_WARPS, THREADS = 32 * (MMA_WARP + 1);
+    static constexpr int OFF_Q = 0, OFF_K = OFF_Q + NT * Q_TILE, OFF_V = OFF_K + STAGES * K_TILE;
+    static constexpr int OFF_FAC = OFF_V + STAGES * V_TILE;     // factor of every row's scores
+    static constexpr int OFF_NAN = OFF_FAC + ROWS * 4;          // 64-bit word per channel, see note_nan
+    static constexpr int OFF_BAR = OFF_NAN + D * 8;
+    static constexpr int OFF_MISC = OFF_BAR + 256;
+    static constexpr int SMEM = OFF_MISC + 64 + 1024;           // the tiles start on a 1,024-byte boundary
+    static_assert(SMEM <= 232448, "shared memory of a block");
+};
+
+// mbarriers (index); phases are counted by the waiting side
+enum {
+    kKFull = 0, kKEmpty = 2, kVFull = 4, kVEmpty = 6,           // [stage]
+    kSFull = 8, kPFull = 10,                                    // [score buffer]
+    kPvDone = 12,                                               // [row tile]
+    kQFull = 14, kFacRead = 15, kSegDone = 16, kDrained = 17, kBars = 18
+};
+
+// ---- the units --------------------------------------------------------------------------------------
+struct Unit { int stale_tiles, fp8_tiles, n_fp8; };
+
+// key tiles of the rows [rt * ROWS, (rt + 1) * ROWS) of a request
+template <int ROWS>
+__device__ __forceinline__ Unit unit_of(const Request& r, int group, int rt)
+{
+    const int last = (min(r.n_new * group, (rt + 1) * ROWS) - 1) / group;
+    const int p = r.len - r.n_new + last;                       // the last position that a row sees
+    Unit u = {0, 0, 0};
+    if (p < 0) return u;
+    const int run = p >> 4, runs = (r.len + 15) >> 4;
+    // FP8 runs behind the last row's position are left out where they are the row's last runs; elsewhere the masks do it
+    u.n_fp8 = r.exact && r.stale_end <= run + 1 ? r.n_fp8 - (runs - 1 - run) : r.n_fp8;
+    u.stale_tiles = (r.n_stale + 7) >> 3;
+    u.fp8_tiles = (u.n_fp8 + 7) >> 3;
+    return u;
+}
+
+struct Segment {
+    Request r;
+    Unit u;
+    int b, h, rt, nt;            // nt: row tiles that hold rows
+    int t0, t1;                  // key tiles of this block, Stale ones first
+    int slot;                    // of the partial, or -1 where the block has the whole unit
+    bool first_part;
+    int last_block;
+};
+
+// Walks the units that the positions [p0, p1) of the cut meet; every thread of a block does so by itself.
+template <int ROWS>
+struct Walker {
+    const Params& P;
+    long long p0, p1, at, per;
+    int b, h, rt, block;
+    Request r;
+
+    __device__ __forceinline__ Walker(const Params& P_, long long p0_, long long p1_, long long per_, int b_, long long request_start)
+        : P(P_), p0(p0_), p1(p1_), at(request_start), per(per_), b(b_), h(0), rt(0), block(blockIdx.x)
+    {
+        r = P.req[b];
+        const long long skip = (p0 - at) / r.cost;              // KV heads before the first unit
+        h = (int)skip;
+        at += skip * r.cost;
+    }
+    __device__ __forceinline__ bool next(Segment& s)
+    {
+        while (at < p1 && b < P.B) {
+            const int n_rt = (r.n_new * P.group + ROWS - 1) / ROWS;
+            if (n_rt == 0) {
+                if (++b < P.B) r = P.req[b];
+                continue;
+            }
+            s.r = r;
+            s.u = unit_of<ROWS>(r, P.group, rt);
+            const int n = s.u.stale_tiles + s.u.fp8_tiles;
+            const long long start = at, first = at + kUnitCost;
+            s.b = b; s.h = h; s.rt = rt;
+            s.nt = min(ROWS / 128, (r.n_new * P.group - rt * ROWS + 127) / 128);
+            at = first + n;
+            if (++rt == n_rt) {
+                rt = 0;
+                if (++h == P.hkv) {
+                    h = 0;
+                    if (++b < P.B) r = P.req[b];
+                }
+            }
+            s.t0 = (int)max(0ll, p0 - first);
+            s.t1 = (int)min((long long)n, p1 - first);
+            if (n == 0) s.t0 = s.t1 = 0;                         // rows that see nothing
+            if (s.t1 > s.t0 || (n == 0 && start >= p0)) {
+                const bool whole = s.t0 == 0 && s.t1 == n;
+                s.slot = whole ? -1 : 2 * block + (start >= p0 ? 1 : 0);
+                s.first_part = !whole && s.t0 == 0;
+                s.last_block = (int)((first + n - 1) / per);
+                return true;
+            }
+        }
+        return false;
+    }
+};
+
+// ---- plan -------------------------------------------------------------------------------------------
+// One block per request: the row's pages by format, in order, and what the cut needs to know.  Bound by latency (a scan
+// of the row's tags, 4,096 pages at a time).
+constexpr int kPlanThreads = 256, kPlanPer = 16;
+
+template <int ROWS>
+__global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const Params P)
+{
+    __shared__ int warp_sum[2][kPlanThreads / 32];
+    __shared__ int bad_s, stale_end_s;
+    __shared__ long long cost_s;
+    pdl_begin();
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int T = P.tiles * kPage;
+    if (tid == 0) { bad_s = 0; stale_end_s = 0; cost_s = 0; }
+    int len = P.lens[b];
+    const int first = P.starts[b], last = P.starts[b + 1];
+    uint32_t flags = 0;
+    if ((long long)len > (long long)P.max_pages * T) { flags = kStBounds; len = P.max_pages * T; }
+    if (len < 0) len = 0;
+    int n_new = last - first;
+    if (first < 0 || last > P.n_rows || n_new < 0) { flags = kStBounds; n_new = 0; }
+    const int pages = n_new > 0 ? (len + T - 1) / T : 0;
+    const int32_t* ids = P.bt + (size_t)b * P.max_pages;
+    const uint8_t* tags = P.tags + (size_t)b * P.max_pages;
+    int2* list = P.list + (size_t)b * P.max_pages;
+    int n_stale = 0, n_fp8 = 0;                                 // pages listed so far
+    __syncthreads();
+    for (int base = 0; base < pages; base += kPlanThreads * kPlanPer) {
+        const int p0 = base + tid * kPlanPer;
+        int id[kPlanPer];
+        uint32_t stale = 0, fp8 = 0;
+#pragma unroll
+        for (int i = 0; i < kPlanPer; ++i) {
+            const int p = p0 + i;
+            if (p >= pages) break;
+            const int tag = tags[p];
+            id[i] = ids[p];
+            const bool is_stale = tag == MKV_TAG_STALE;
+            const bool ok = is_stale ? id[i] >= 0 && id[i] < P.tq3_pages && (long long)(p + 1) * T <= len
+                                     : tag <= MKV_TAG_ANCHOR && id[i] >= 0 && id[i] < P.fp8_pages;
+            if (!ok) flags |= kStBounds;                        // never dereferenced
+            else if (is_stale) stale |= 1u << i;
+            else fp8 |= 1u << i;
+        }
+        const int c3 = __popc(stale), c8 = __popc(fp8);
+        int s3 = c3, s8 = c8;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int a = __shfl_up_sync(0xffffffffu, s3, o), c = __shfl_up_sync(0xffffffffu, s8, o);
+            if (lane >= o) { s3 += a; s8 += c; }
+        }
+        if (lane == 31) { warp_sum[0][warp] = s3; warp_sum[1][warp] = s8; }
+        __syncthreads();
+        int at3 = n_stale + s3 - c3, at8 = n_fp8 + s8 - c8;
+#pragma unroll
+        for (int w = 0; w < kPlanThreads / 32; ++w) {
+            if (w < warp) { at3 += warp_sum[0][w]; at8 += warp_sum[1][w]; }
+            n_stale += warp_sum[0][w];
+            n_fp8 += warp_sum[1][w];
+        }
+#pragma unroll
+        for (int i = 0; i < kPlanPer; ++i) {
+            if (stale >> i & 1) list[at3++] = make_int2(p0 + i, id[i]);
+            else if (fp8 >> i & 1) list[P.max_pages - 1 - at8++] = make_int2(p0 + i, id[i]);
+        }
+        if (stale) atomicMax(&stale_end_s, (p0 + 32 - __clz(stale)) * P.tiles);
+        __syncthreads();
+    }
+    if (flags) {
+        bad_s = 1;
+        atomicOr(P.status, flags);
+    }
+    __syncthreads();
+    Request r;
+    r.n_new = n_new; r.row0 = first; r.len = len; r.pad = 0;
+    r.n_stale = n_stale * P.tiles;
+    r.n_fp8 = n_fp8 * P.tiles;
+    // an open last page counts its filled runs (an open page is FP8, or it is in no list)
+    r.exact = !bad_s;
+    if (pages > 0 && n_fp8 > 0 && list[P.max_pages - n_fp8].x == pages - 1)
+        r.n_fp8 -= P.tiles - ((len - (pages - 1) * T + kPage - 1) / kPage);
+    r.stale_end = stale_end_s;
+    const int n_rt = (n_new * P.group + ROWS - 1) / ROWS;
+    long long cost = 0;
+    for (int rt = tid; rt < n_rt; rt += kPlanThreads) {
+        const Unit u = unit_of<ROWS>(r, P.group, rt);
+        cost += u.stale_tiles + u.fp8_tiles + kUnitCost;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) cost += __shfl_xor_sync(0xffffffffu, cost, o);
+    if (lane == 0 && cost) atomicAdd(reinterpret_cast<unsigned long long*>(&cost_s), (unsigned long long)cost);
+    __syncthreads();
+    if (tid == 0) {
+        r.cost = cost_s;
+        P.req[b] = r;
+    }
+}
+
+// ---- shared-memory operands and tensor-memory access ----------------------------------------------------
+// K-major operand with the 128-byte swizzle: rows of 64 fp16, eight rows 1,024 bytes; the 16-byte chunk c of row r sits
+// at chunk c ^ (r mod 8).  Successive 64-element atoms are a whole operand column apart.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t saddr)
+{
+    return (uint64_t)((saddr >> 4) & 0x3FFF) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
+           ((uint64_t)2 << 61);
+}
+__device__ __forceinline__ uint32_t chunk_at(int row, int c) { return (uint32_t)(row * 128 + ((c ^ (row & 7)) << 4)); }
+__host__ __device__ constexpr uint32_t idesc(int n) { return (1u << 4) | (uint32_t)(n >> 3) << 17 | (uint32_t)(128 >> 4) << 24; }   // f16 x f16 -> f32, M 128
+
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void sts64(uint32_t addr, uint32_t a, uint32_t b)
+{
+    asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+}
+__device__ __forceinline__ void sts32(uint32_t addr, uint32_t a) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(a) : "memory"); }
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+}
+// 32 columns of the thread's tensor-memory lane
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&r)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+                 "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]),
+                   "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]),
+                   "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]),
+                   "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+                 : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&r)[32])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+                 "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+                 ::"r"(taddr), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]),
+                   "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]), "f"(r[14]), "f"(r[15]), "f"(r[16]), "f"(r[17]),
+                   "f"(r[18]), "f"(r[19]), "f"(r[20]), "f"(r[21]), "f"(r[22]), "f"(r[23]), "f"(r[24]), "f"(r[25]), "f"(r[26]),
+                   "f"(r[27]), "f"(r[28]), "f"(r[29]), "f"(r[30]), "f"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+                   "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ uint32_t hmul2_u32(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// true where one of the two fp16 is NaN
+__device__ __forceinline__ bool has_nan2(uint32_t x)
+{
+    const __half2 h = *reinterpret_cast<const __half2*>(&x);
+    return __hisnan(__low2half(h)) || __hisnan(__high2half(h));
+}
+__device__ __forceinline__ uint4 ldg128(const void* p)          // coherent: pages may have been written by the kernel before
+{
+    uint4 v;
+    asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint2 ldg64(const void* p)
+{
+    uint2 v;
+    asm volatile("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint32_t ldg32(const void* p)
+{
+    uint32_t v;
+    asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+
+// four key levels of record format 2 from four nibbles (the fp16 levels 3400, 3A00, 3D80, 4080 | sign)
+__device__ __forceinline__ void key_lut4_v2(uint32_t sel, uint32_t& r0, uint32_t& r1)
+{
+    const uint32_t hi = prmt(0x403D3A34u, 0xC0BDBAB4u, sel);
+    const uint32_t lo = prmt(0x80800000u, 0x80800000u, sel);
+    r0 = prmt(lo, hi, 0x5140u);
+    r1 = prmt(lo, hi, 0x7362u);
+}
+
+// Key row of token t of the run e in a tile: FP8 tiles keep the order; Stale tiles follow the lanes of the value codes,
+// which hold tokens 2q, 2q + 1, 2q + 8, 2q + 9 of a run: two runs' shares are one 16-byte chunk, chunk 2q + (pair mod 2).
+__device__ __forceinline__ int stale_row(int e, int t)
+{
+    return 64 * (e >> 2) + 8 * (2 * ((t & 7) >> 1) + ((e >> 1) & 1)) + 4 * (e & 1) + 2 * (t >> 3) + (t & 1);
+}
+// ... and back: run and token of key row n
+__device__ __forceinline__ int run_of_row(int n) { return 4 * (n >> 6) + 2 * ((n >> 3) & 1) + ((n >> 2) & 1); }
+__device__ __forceinline__ int token_of_row(int n) { return 2 * ((n >> 4) & 3) + (n & 1) + 8 * ((n >> 1) & 1); }
+
+// ---- scan -------------------------------------------------------------------------------------------
+template <int D, int FMT>
+__global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Params P)
+{
+    using G = Geo<D>;
+    using namespace tm;
+    constexpr int NT = G::NT, ROWS = G::ROWS;
+    constexpr uint32_t FULL = 0xffffffffu;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const uint32_t sb = smem_u32(smem);
+    float* fac_s = reinterpret_cast<float*>(smem + G::OFF_FAC);
+    unsigned long long* nan_s = reinterpret_cast<unsigned long long*>(smem + G::OFF_NAN);
+    volatile int* failed_s = reinterpret_cast<volatile int*>(smem + G::OFF_MISC);
+    uint32_t* tmem_s = reinterpret_cast<uint32_t*>(smem + G::OFF_MISC + 4);
+    int* start_b_s = reinterpret_cast<int*>(smem + G::OFF_MISC + 8);
+    long long* start_s = reinterpret_cast<long long*>(smem + G::OFF_MISC + 16);   // request's first position, total
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    auto bar = [&](int i) -> uint32_t { return sb + G::OFF_BAR + 8 * i; };
+
+    if (tid == 0) {
+        for (int i = 0; i < kBars; ++i) {
+            int count = 1;
+            if ((i >= kKFull && i < kKEmpty) || (i >= kVFull && i < kVEmpty) || i == kQFull) count = G::UNPACK_WARPS;
+            else if (i >= kPFull && i < kPvDone) count = 4;
+            else if (i == kFacRead || i == kSegDone) count = G::SOFT_WARPS;
+            mbar_init(bar(i), count);
+        }
+        *failed_s = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    for (int i = tid; i < D; i += G::THREADS) nan_s[i] = 0;
+    pdl_wait();
+    // ---- the block's share: [p0, p1) of the units laid end to end
+    if (warp == 0) {
+        long long total = 0;
+        for (int i = lane; i < P.B; i += 32) total += P.req[i].cost;
+        total *= P.hkv;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(FULL, total, o);
+        const long long per = max((total + gridDim.x - 1) / gridDim.x, (long long)(kLeastShare + kUnitCost));
+        const long long p0 = per * blockIdx.x;
+        long long before = 0, at = 0;
+        int found = -1;
+        for (int i0 = 0; i0 < P.B && p0 < total && found < 0; i0 += 32) {
+            const long long c = i0 + lane < P.B ? P.req[i0 + lane].cost * P.hkv : 0;
+            long long s = c;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long a = __shfl_up_sync(FULL, s, o);
+                if (lane >= o) s += a;
+            }
+            const uint32_t m = __ballot_sync(FULL, before + s > p0);
+            if (m) {
+                const int src = __ffs(m) - 1;
+                found = i0 + src;
+                at = before + __shfl_sync(FULL, s - c, src);
+            }
+            before += __shfl_sync(FULL, s, 31);
+        }
+        if (lane == 0) {
+            *start_b_s = found;
+            start_s[0] = at;
+            start_s[1] = total;
+            start_s[2] = per;
+        }
+    }
+    __syncthreads();
+    const int b0 = *start_b_s;
+    const long long total = start_s[1], per = start_s[2];
+    if (tid == 0) P.merge[blockIdx.x].b = -1;
+    if (b0 < 0) return;                                          // nothing to do (and nothing allocated yet)
+    if (warp == G::MMA_WARP) tmem_alloc(smem_u32(tmem_s), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tb = *tmem_s;
+    constexpr uint32_t kColS = NT * D;                           // O: NT x D columns, then two score buffers
+    const long long p0 = per * blockIdx.x, p1 = min(total, p0 + per);
+    Walker<ROWS> walk(P, p0, p1, per, b0, start_s[0]);
+    Segment s;
+
+    // bounded by wall time: a wait that gives up flags the pool and lets every later wait of the block pass
+    auto wait = [&](int i, uint32_t parity) {
+        const uint32_t a = bar(i);
+        if (mbar_try_wait(a, parity)) return;
+        unsigned long long t0 = 0, t1;
+        for (int spins = 1; !*failed_s; ++spins) {
+            if (mbar_try_wait(a, parity)) return;
+            if ((spins & 63) == 0) {
+                asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));
+                if (t0 == 0) t0 = t1;
+                if (t1 - t0 > P.wait_ns) {
+                    *failed_s = 1;
+                    atomicOr(P.status, kStTimeout);
+                }
+            }
+        }
+    };
+
+    if (warp == G::MMA_WARP) {
+        // ================= products =================
+        if (lane == 0) {
+            uint32_t job = 0, tile = 0, fills = 0;               // scores, key tiles and queries so far
+            while (walk.next(s)) {
+                const int n = (s.t1 - s.t0) * s.nt, cut = s.u.stale_tiles;
+                auto scores = [&](int i) {                       // job i of the segment: key tile t0 + i / nt, row tile i % nt
+                    const int j = i / s.nt, t = i - j * s.nt, kt = s.t0 + j;
+                    const uint32_t at = tile + j, st = at % G::STAGES, buf = (job + i) & 1;
+                    if (t == 0) {
+                        if (j == 0 || kt == cut) wait(kQFull, fills++ & 1);
+                        wait(kKFull + st, (at / G::STAGES) & 1);
+                        tc_fence_after();
+                    }
+                    const uint64_t a = operand_desc(sb + G::OFF_Q + t * G::Q_TILE), k = operand_desc(sb + G::OFF_K + st * G::K_TILE);
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint64_t step = ((kk >> 2) * (128 * 128) + (kk & 3) * 32) >> 4;
+                        mma_ss(tb + kColS + kKeys * buf, a + step, k + step, idesc(kKeys), kk > 0);
+                    }
+                    mma_commit(bar(kSFull + buf));
+                    if (t == s.nt - 1) mma_commit(bar(kKEmpty + st));
+                };
+                if (n > 0) scores(0);
+                if (n > 1) scores(1);
+                for (int i = 0; i < n; ++i) {
+                    const int j = i / s.nt, t = i - j * s.nt;
+                    const uint32_t at = tile + j, st = at % G::STAGES, buf = (job + i) & 1;
+                    if (t == 0) wait(kVFull + st, (at / G::STAGES) & 1);
+                    wait(kPFull + buf, ((job + i) >> 1) & 1);
+                    tc_fence_after();
+                    const uint64_t v = operand_desc(sb + G::OFF_V + st * G::V_TILE);
+#pragma unroll
+                    for (int kk = 0; kk < kKeys / 16; ++kk)
+                        mma_ts(tb + t * D, tb + kColS + kKeys * buf + 8 * kk, v + (((kk >> 2) * (D * 128) + (kk & 3) * 32) >> 4), idesc(D),
+                               j > 0 || kk > 0);
+                    mma_commit(bar(kPvDone + t));
+                    if (t == s.nt - 1) mma_commit(bar(kVEmpty + st));
+                    if (i + 2 < n) scores(i + 2);
+                }
+                job += n;
+                tile += s.t1 - s.t0;
+            }
+            // tensor memory is given back when nothing writes it any more (also after a wait that gave up; bounded again)
+            mma_commit(bar(kDrained));
+            unsigned long long t0, t1;
+            asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+            while (!mbar_try_wait(bar(kDrained), 0)) {
+                asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));
+                if (t1 - t0 > 20000000ull) {
+                    atomicOr(P.status, kStTimeout);
+                    break;
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp >= G::SOFT_WARPS) {
+        // ================= queries and unpacking =================
+        const int w = warp - G::SOFT_WARPS, g = lane >> 2, tq = lane & 3;
+        const uint32_t ku = (uint32_t)(15 - P.ke) << 10, vu = (uint32_t)(15 - P.ve) << 10;     // 2^-ke, 2^-ve as fp16
+        const uint32_t k_unit = ku | ku << 16, v_unit = vu | vu << 16;
+        uint32_t tile = 0, fills = 0, segments = 0;
+        auto arrive = [&](int i) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(i));
+        };
+        while (walk.next(s)) {
+            ++segments;
+            const int first_pos = s.r.len - s.r.n_new + s.rt * ROWS / P.group;        // of the unit's first row
+            const int rows = min(ROWS, s.r.n_new * P.group - s.rt * ROWS);
+            const int2* list = P.list + (size_t)s.b * P.max_pages;
+            const size_t page8 = fp8_page_bytes(D, P.tiles), page3 = tq3_page_bytes(D, P.tiles);
+            const uint8_t* base8 = P.fp8 + s.h * page8;
+            const uint8_t* base3 = P.tq3 + s.h * page3;
+
+            // ---- queries of one format: a warp per row, a lane D / 32 dims
+            auto fill_query = [&](bool stale) {
+                if (tile > 0) wait(kKEmpty + (tile - 1) % G::STAGES, ((tile - 1) / G::STAGES) & 1);   // the products so far are done
+                if (fills > 0) wait(kFacRead, (fills - 1) & 1);
+                ++fills;
+                constexpr int N = D / 32;
+                for (int r0 = w * 4; r0 < s.nt * 128; r0 += 4 * G::UNPACK_WARPS) {
+                    uint32_t raw[4][N / 2];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const int r = r0 + u, row = s.rt * ROWS + r, tok = row / P.group;
+#pragma unroll
+                        for (int i = 0; i < N / 2; ++i) raw[u][i] = 0;
+                        if (r < rows) {
+                            const __nv_bfloat16* src = P.q + (size_t)(s.r.row0 + tok) * P.q_stride +
+                                                       (size_t)(s.h * P.group + row - tok * P.group) * D + lane * N;
+                            if constexpr (N == 8) {
+                                const uint4 v = ldg128(src);
+                                raw[u][0] = v.x; raw[u][1] = v.y; raw[u][2] = v.z; raw[u][3] = v.w;
+                            } else {
+                                const uint2 v = ldg64(src);
+                                raw[u][0] = v.x; raw[u][1] = v.y;
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const int r = r0 + u;
+                        float x[N];
+#pragma unroll
+                        for (int i = 0; i < N / 2; ++i) {
+                            x[2 * i] = __uint_as_float(raw[u][i] << 16);
+                            x[2 * i + 1] = __uint_as_float(raw[u][i] & 0xffff0000u);
+                        }
+                        if (stale) {
+#pragma unroll
+                            for (int i = 0; i < N; ++i) {
+                                const int dim = lane * N + i;
+                                if ((P.sigma.w[dim >> 5] >> (dim & 31)) & 1u) x[i] = -x[i];
+                            }
+#pragma unroll
+                            for (int hh = 1; hh < N; hh <<= 1)
+#pragma unroll
+                                for (int i = 0; i < N; ++i)
+                                    if ((i & hh) == 0) {
+                                        const float p = x[i], q = x[i + hh];
+                                        x[i] = p + q;
+                                        x[i + hh] = p - q;
+                                    }
+#pragma unroll
+                            for (int m = 1; m < 32; m <<= 1)
+#pragma unroll
+                                for (int i = 0; i < N; ++i) {
+                                    const float o = __shfl_xor_sync(FULL, x[i], m);
+                                    x[i] = (lane & m) ? o - x[i] : x[i] + o;
+                                }
+                            const float rs = D == 256 ? 0.0625f : 0.08838834764831845f;        // d^-1/2
+#pragma unroll
+                            for (int i = 0; i < N; ++i) x[i] *= rs;
+                        }
+                        // a power of two brings the largest element to [1/2, 1): exact for the plain query
+                        float big = 0.f;
+#pragma unroll
+                        for (int i = 0; i < N; ++i) big = fmaxf(big, fabsf(x[i]));
+#pragma unroll
+                        for (int m = 16; m > 0; m >>= 1) big = fmaxf(big, __shfl_xor_sync(FULL, big, m));
+                        int e = (int)(__float_as_uint(big) >> 23) - 126;
+                        if (e < -100 || e > 100) e = 0;                                        // nothing but zeros, or infinities
+                        const float down = __uint_as_float((uint32_t)(127 - e) << 23), up = __uint_as_float((uint32_t)(127 + e) << 23);
+                        const float sg = P.negative ? -down : down;
+                        uint32_t h2[N / 2];
+#pragma unroll
+                        for (int i = 0; i < N / 2; ++i) h2[i] = pack_f16x2(x[2 * i] * sg, x[2 * i + 1] * sg);
+                        if (lane == 0)
+                            fac_s[r] = fmaxf(P.sc2 * up * (stale ? __uint_as_float((uint32_t)(127 + P.ke) << 23) : P.k_scale), 1e-30f);
+                        const uint32_t row_at = sb + G::OFF_Q + (r >> 7) * G::Q_TILE;
+                        const int rr = r & 127, d0 = lane * N;
+                        if (!stale) {
+                            const uint32_t a = row_at + (d0 >> 6) * (128 * 128) + chunk_at(rr, (d0 & 63) >> 3);
+                            if constexpr (N == 8) sts128(a, h2[0], h2[1], h2[2], h2[3]);
+                            else sts64(a + (d0 & 7) * 2, h2[0], h2[1]);
+                        } else if constexpr (FMT == 2) {
+                            // dims 4 q .. 4 q + 3 (+ 16) of a 32-dim step: chunk 2 q + step, elements 4 (k / 16) ..
+#pragma unroll
+                            for (int i = 0; i < N; i += 4) {
+                                const int dim = d0 + i, k = dim & 31;
+                                const int c = 2 * ((k & 15) >> 2) + ((dim >> 5) & 1);
+                                sts64(row_at + (dim >> 6) * (128 * 128) + chunk_at(rr, c) + 8 * (k >> 4), h2[i / 2], h2[i / 2 + 1]);
+                            }
+                        } else {
+                            // dims 2 q, 2 q + 1 (+ 8) of a 16-dim block: chunk 2 q + (block / 2 mod 2), elements 4 (block mod 2) ..
+#pragma unroll
+                            for (int i = 0; i < N; i += 2) {
+                                const int dim = d0 + i, sl = dim & 15, kb = (dim >> 4) & 3;
+                                const int c = 2 * ((sl & 7) >> 1) + (kb >> 1);
+                                sts32(row_at + (dim >> 6) * (128 * 128) + chunk_at(rr, c) + 8 * (kb & 1) + 4 * (sl >> 3), h2[i / 2]);
+                            }
+                        }
+                    }
+                }
+                arrive(kQFull);
+            };
+
+            // A value that is NaN is as a rule seen by every row of the tile (0 x NaN).  In a tile with masked places it
+            // is taken out and its channel's first such position noted; the epilogue gives NaN to the rows from there
+            // on.  The note carries the segment, and an older segment's epilogue is waited for before it is replaced.
+            auto note_nan = [&](int channel, int pos) {
+                if (segments > 1) wait(kSegDone, (segments - 2) & 1);
+                atomicMax(&nan_s[channel], (unsigned long long)segments << 32 | (uint32_t)(kNoPos - pos));
+            };
+
+            const int cut = s.u.stale_tiles;
+            if (s.t0 < cut) {
+                // ---- Stale tiles: keys of run w; values of the two runs w & ~1, w | 1, half of the channels
+                constexpr int LW = 3 * D / 64;                   // packed words of a lane per section
+                const int n_tiles = min(s.t1, cut);
+                const int half = w & 1;
+                const uint8_t *rec[2], *meta[2];                 // the pair's records (null: no run) and page scales
+                int pos[2];
+                auto locate = [&](int t) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int run = t * 8 + (w & ~1) + e;
+                        rec[e] = nullptr;
+                        if (t < n_tiles && run < s.r.n_stale) {
+                            const int pg = run / P.tiles, sub = run - pg * P.tiles;
+                            const int2 entry = list[pg];
+                            const uint8_t* page = base3 + (size_t)entry.y * P.hkv * page3;
+                            rec[e] = page + (size_t)sub * tq3_tile_bytes(D);
+                            meta[e] = page + (size_t)P.tiles * tq3_tile_bytes(D);
+                            pos[e] = (entry.x * P.tiles + sub) * kPage;
+                        }
+                    }
+                };
+                uint32_t kw[LW], gw, vw[2][LW / 2 + (LW / 2 & 1)], mw[2][D / 32][2];
+                auto load_keys = [&] {
+                    const uint8_t* r = rec[half];
+                    if (!r) {
+#pragma unroll
+                        for (int i = 0; i < LW; ++i) kw[i] = 0;
+                        gw = 0;
+                        return;
+                    }
+#pragma unroll
+                    for (int c = 0; c < LW / 4; ++c) {
+                        const uint4 v = ldg128(r + c * 512 + lane * 16);
+                        kw[4 * c] = v.x; kw[4 * c + 1] = v.y; kw[4 * c + 2] = v.z; kw[4 * c + 3] = v.w;
+                    }
+                    if constexpr (LW % 4 != 0) {
+                        const uint2 v = ldg64(r + (LW / 4) * 512 + lane * 8);
+                        kw[LW - 2] = v.x; kw[LW - 1] = v.y;
+                    }
+                    // g of tokens g and g + 8
+                    const __half* gp = reinterpret_cast<const __half*>(r + 12 * D);
+                    gw = (uint32_t)*reinterpret_cast<const volatile uint16_t*>(gp + g) |
+                         (uint32_t)*reinterpret_cast<const volatile uint16_t*>(gp + g + 8) << 16;
+                };
+                auto load_values = [&] {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        if (!rec[e]) {
+#pragma unroll
+                            for (int i = 0; i < (int)(sizeof vw[0] / 4); ++i) vw[e][i] = 0;
+#pragma unroll
+                            for (int i = 0; i < D / 32; ++i) mw[e][i][0] = mw[e][i][1] = 0;
+                            continue;
+                        }
+                        const uint8_t* v = rec[e] + 6 * D;
+                        if constexpr (D == 256) {                // words 0-5 or 6-11 of the lane
+                            if (half == 0) {
+                                const uint4 a = ldg128(v + lane * 16);
+                                const uint2 c = ldg64(v + 512 + lane * 16);
+                                vw[e][0] = a.x; vw[e][1] = a.y; vw[e][2] = a.z; vw[e][3] = a.w; vw[e][4] = c.x; vw[e][5] = c.y;
+                            } else {
+                                const uint2 a = ldg64(v + 512 + lane * 16 + 8);
+                                const uint4 c = ldg128(v + 1024 + lane * 16);
+                                vw[e][0] = a.x; vw[e][1] = a.y; vw[e][2] = c.x; vw[e][3] = c.y; vw[e][4] = c.z; vw[e][5] = c.w;
+                            }
+                        } else {                                 // words 0-2 or 3-5
+                            if (half == 0) {
+                                const uint4 a = ldg128(v + lane * 16);
+                                vw[e][0] = a.x; vw[e][1] = a.y; vw[e][2] = a.z;
+                            } else {
+                                const uint32_t a = ldg32(v + lane * 16 + 12);
+                                const uint2 c = ldg64(v + 512 + lane * 8);
+                                vw[e][0] = a; vw[e][1] = c.x; vw[e][2] = c.y;
+                            }
+                        }
+                        // scale / zero of the block pairs of these channels: (sc g, sc g+8), (zp g, zp g+8), twice
+#pragma unroll
+                        for (int i = 0; i < D / 64; ++i) {
+                            const uint4 m = ldg128(meta[e] + (half * (D / 64) + i) * 128 + g * 16);
+                            mw[e][2 * i][0] = m.x; mw[e][2 * i][1] = m.y; mw[e][2 * i + 1][0] = m.z; mw[e][2 * i + 1][1] = m.w;
+                        }
+                    }
+                };
+                locate(s.t0);
+                load_keys();
+                load_values();
+                fill_query(true);
+                for (int t = s.t0; t < n_tiles; ++t, ++tile) {
+                    const uint32_t st = tile % G::STAGES, ph = (tile / G::STAGES) & 1;
+                    if (tile >= G::STAGES) wait(kKEmpty + st, ph ^ 1);
+                    const uint32_t k_at = sb + G::OFF_K + st * G::K_TILE;
+                    {
+                        const int n0 = stale_row(w, g), n1 = stale_row(w, g + 8);
+                        const uint32_t g0 = hmul2_u32(prmt(gw, gw, 0x1010u), k_unit), g1 = hmul2_u32(prmt(gw, gw, 0x3232u), k_unit);
+#pragma unroll
+                        for (int j = 0; j < D / 64; ++j) {
+                            const uint32_t A = kw[3 * j], Bw = kw[3 * j + 1], Cw = kw[3 * j + 2];
+                            uint32_t sel[4];
+                            sel[0] = A & 0x77777777u;
+                            sel[1] = Bw & 0x77777777u;
+                            sel[2] = lop3_and_or(A >> 1, 0x44444444u, Cw & 0x33333333u);
+                            sel[3] = lop3_and_or(Bw >> 1, 0x44444444u, (Cw >> 2) & 0x33333333u);
+                            const uint32_t at = k_at + j * (kKeys * 128);
+#pragma unroll
+                            for (int c = 0; c < 2; ++c) {
+                                uint32_t lo[4], hi[4];           // chunk of token g, of token g + 8
+                                if constexpr (FMT == 2) {
+                                    key_lut4_v2(sel[2 * c], lo[0], lo[1]);
+                                    key_lut4_v2(sel[2 * c] >> 16, lo[2], lo[3]);
+                                    key_lut4_v2(sel[2 * c + 1], hi[0], hi[1]);
+                                    key_lut4_v2(sel[2 * c + 1] >> 16, hi[2], hi[3]);
+                                } else {
+                                    key_lut4(sel[2 * c], lo[0], hi[0]);
+                                    key_lut4(sel[2 * c] >> 16, lo[1], hi[1]);
+                                    key_lut4(sel[2 * c + 1], lo[2], hi[2]);
+                                    key_lut4(sel[2 * c + 1] >> 16, lo[3], hi[3]);
+                                }
+                                sts128(at + chunk_at(n0, 2 * tq + c), hmul2_u32(lo[0], g0), hmul2_u32(lo[1], g0), hmul2_u32(lo[2], g0), hmul2_u32(lo[3], g0));
+                                sts128(at + chunk_at(n1, 2 * tq + c), hmul2_u32(hi[0], g1), hmul2_u32(hi[1], g1), hmul2_u32(hi[2], g1), hmul2_u32(hi[3], g1));
+                            }
+                        }
+                    }
+                    arrive(kKFull + st);
+                    const bool masked = t * 8 + 8 > s.r.n_stale || s.r.stale_end * kPage > first_pos + 1;
+                    const bool had[2] = {rec[0] != nullptr, rec[1] != nullptr};
+                    const int at_pos[2] = {pos[0], pos[1]};
+                    locate(t + 1);
+                    load_keys();
+                    if (tile >= G::STAGES) wait(kVEmpty + st, ph ^ 1);
+                    const uint32_t v_at = sb + G::OFF_V + st * G::V_TILE + (w >> 2) * (D * 128);
+                    const int c = 2 * tq + ((w >> 1) & 1);
+#pragma unroll
+                    for (int j = 0; j < D / 128; ++j) {          // 64 channels: four blocks of 16
+                        uint32_t X0[2], X1[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            X0[e] = prmt(vw[e][3 * j], vw[e][3 * j + 1], 0x6341u);
+                            X1[e] = prmt(vw[e][3 * j + 1], vw[e][3 * j + 2], 0x6341u);
+                        }
+#pragma unroll
+                        for (int blk = 0; blk < 4; ++blk) {
+                            uint32_t o[2][4];                    // run e: row g (tokens low, high), row g + 8 (low, high)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const uint32_t W0 = vw[e][3 * j], W1 = vw[e][3 * j + 1], W2 = vw[e][3 * j + 2];
+                                uint32_t a[4];
+                                if (blk == 0) value_operands<0>(a, W0, W1, W2, X0[e]);
+                                else if (blk == 1) value_operands<1>(a, W0, W1, W2, X0[e]);
+                                else if (blk == 2) value_operands<2>(a, W0, W1, W2, X1[e]);
+                                else value_operands<3>(a, W0, W1, W2, X1[e]);
+                                const uint32_t sc = hmul2_u32(mw[e][4 * j + blk][0], v_unit), zp = hmul2_u32(mw[e][4 * j + blk][1], v_unit);
+                                const uint32_t s0 = prmt(sc, sc, 0x1010u), s1 = prmt(sc, sc, 0x3232u);
+                                const uint32_t z0 = prmt(zp, zp, 0x1010u), z1 = prmt(zp, zp, 0x3232u);
+                                o[e][0] = hfma2_u32(a[0], s0, z0);
+                                o[e][1] = hfma2_u32(a[2], s0, z0);
+                                o[e][2] = hfma2_u32(a[1], s1, z1);
+                                o[e][3] = hfma2_u32(a[3], s1, z1);
+                            }
+                            const int ch = half * (D / 2) + 64 * j + 16 * blk + g;
+                            if (masked) {
+#pragma unroll
+                                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i)
+                                        if (had[e] && has_nan2(o[e][i])) {         // a scale or zero that is not a number
+                                            note_nan(ch + 8 * (i >> 1), at_pos[e] + 2 * tq + 8 * (i & 1));
+                                            o[e][i] = 0;
+                                        }
+                            }
+                            sts128(v_at + chunk_at(ch, c), o[0][0], o[0][1], o[1][0], o[1][1]);
+                            sts128(v_at + chunk_at(ch + 8, c), o[0][2], o[0][3], o[1][2], o[1][3]);
+                        }
+                    }
+                    arrive(kVFull + st);
+                    load_values();
+                }
+            }
+            if (s.t1 > cut) {
+                // ---- FP8 tiles: a warp per run
+                constexpr int N = 16 * D / 512;                  // 16-byte loads of a lane for a run's keys, or values
+                const uint8_t* rec;
+                int pos;
+                auto locate = [&](int t) {
+                    const int run = (t - cut) * 8 + w;
+                    rec = nullptr;
+                    if (t < s.t1 && run < s.u.n_fp8) {
+                        const int pg = run / P.tiles, sub = run - pg * P.tiles;
+                        const int2 entry = list[P.max_pages - 1 - pg];
+                        rec = base8 + (size_t)entry.y * P.hkv * page8 + (size_t)sub * fp8_record_bytes(D);
+                        pos = (entry.x * P.tiles + sub) * kPage;
+                    }
+                };
+                uint4 kr[N], vr[N];
+                auto load = [&](uint4 (&x)[N], int off) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) x[i] = rec ? ldg128(rec + off + i * 512 + lane * 16) : make_uint4(0, 0, 0, 0);
+                };
+                const int t_first = max(s.t0, cut);
+                locate(t_first);
+                load(kr, 0);
+                load(vr, 16 * D);
+                fill_query(false);
+                for (int t = t_first; t < s.t1; ++t, ++tile) {
+                    const uint32_t st = tile % G::STAGES, ph = (tile / G::STAGES) & 1;
+                    if (tile >= G::STAGES) wait(kKEmpty + st, ph ^ 1);
+                    const uint32_t k_at = sb + G::OFF_K + st * G::K_TILE;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const int off = i * 512 + lane * 16, tok = off / D, dim = off % D, row = 16 * w + tok;
+                        const uint32_t x[4] = {kr[i].x, kr[i].y, kr[i].z, kr[i].w};
+                        uint32_t o[8];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            o[2 * q] = e4m3x2_to_f16x2((uint16_t)(x[q] & 0xffffu));
+                            o[2 * q + 1] = e4m3x2_to_f16x2((uint16_t)(x[q] >> 16));
+                        }
+                        // chunks c, c + 1; of eight lanes of a row four store them in turned order (bank conflicts)
+                        const uint32_t at = k_at + (dim >> 6) * (kKeys * 128);
+                        const int c = (dim & 63) >> 3;
+                        const bool turn = lane & 4;
+                        sts128(at + chunk_at(row, turn ? c + 1 : c), turn ? o[4] : o[0], turn ? o[5] : o[1], turn ? o[6] : o[2], turn ? o[7] : o[3]);
+                        sts128(at + chunk_at(row, turn ? c : c + 1), turn ? o[0] : o[4], turn ? o[1] : o[5], turn ? o[2] : o[6], turn ? o[3] : o[7]);
+                    }
+                    arrive(kKFull + st);
+                    const int left = rec ? s.r.len - pos : 0;    // tokens of the run that exist
+                    const int this_pos = pos;
+                    const bool masked = rec && pos + kPage - 1 > first_pos;
+                    locate(t + 1);
+                    load(kr, 0);
+                    if (tile >= G::STAGES) wait(kVEmpty + st, ph ^ 1);
+                    const uint32_t v_at = sb + G::OFF_V + st * G::V_TILE + (w >> 2) * (D * 128);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const int ch = i * 32 + lane, c = 2 * (w & 3);
+                        uint32_t x[4] = {vr[i].x, vr[i].y, vr[i].z, vr[i].w};
+                        if (left < kPage) {                      // what no token fills may be anything
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                const int keep = left - 4 * q;
+                                x[q] &= keep >= 4 ? FULL : keep <= 0 ? 0u : (1u << (8 * keep)) - 1u;
+                            }
+                        }
+                        uint32_t o[8];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            o[2 * q] = e4m3x2_to_f16x2((uint16_t)(x[q] & 0xffffu));
+                            o[2 * q + 1] = e4m3x2_to_f16x2((uint16_t)(x[q] >> 16));
+                        }
+                        if (masked) {
+#pragma unroll
+                            for (int q = 0; q < 8; ++q)
+                                if (has_nan2(o[q])) {
+                                    const __half2 h = *reinterpret_cast<const __half2*>(&o[q]);
+                                    const bool low = __hisnan(__low2half(h));
+                                    note_nan(ch, this_pos + 2 * q + (low ? 0 : 1));
+                                    o[q] &= (low ? 0xffff0000u : FULL) & (__hisnan(__high2half(h)) ? 0x0000ffffu : FULL);
+                                }
+                        }
+                        sts128(v_at + chunk_at(ch, c), o[0], o[1], o[2], o[3]);
+                        sts128(v_at + chunk_at(ch, c + 1), o[4], o[5], o[6], o[7]);
+                    }
+                    arrive(kVFull + st);
+                    load(vr, 16 * D);
+                }
+            }
+        }
+    } else {
+        // ================= softmax and output =================
+        const int t = warp >> 2;                                 // row tile
+        const uint32_t my_lanes = (uint32_t)(32 * (warp & 3)) << 16;
+        const int my_row = t * 128 + (warp & 3) * 32 + lane;     // within the unit
+        const uint32_t col_o = tb + my_lanes + t * D;
+        uint32_t job = 0, fills = 0, done = 0, segments = 0;     // done: products with the values so far on this row tile
+        auto warp_arrive = [&](int i) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(i));
+        };
+        while (walk.next(s)) {
+            ++segments;
+            const int row = s.rt * ROWS + my_row, n_rows = s.r.n_new * P.group;
+            const bool live = row < n_rows, warp_live = row - lane < n_rows;
+            const int tok = row / P.group, head = s.h * P.group + row - tok * P.group;
+            const int qpos = s.r.len - s.r.n_new + tok;
+            const int first_pos = s.r.len - s.r.n_new + (s.rt * ROWS + t * 128) / P.group;
+            const int2* list = P.list + (size_t)s.b * P.max_pages;
+            const int cut = s.u.stale_tiles, runs = (s.r.len + 15) >> 4;
+            const bool ordinary = s.r.exact && s.r.stale_end * kPage <= first_pos + 1;     // every Stale page lies before the first row
+            float ref = -CUDART_INF_F, sum = 0.f, fac = 0.f;
+            int n_done = 0;                                      // key tiles of this segment so far
+            for (int kt = s.t0; kt < s.t1; ++kt) {
+                const bool stale = kt < cut;
+                bool turn = false;                               // from Stale values' unit to the FP8 values'
+                if (kt == s.t0 || kt == cut) {
+                    wait(kQFull, fills++ & 1);
+                    fac = fac_s[my_row];
+                    warp_arrive(kFacRead);
+                    turn = kt > s.t0 && P.v_scale != __uint_as_float((uint32_t)(127 + P.ve) << 23);
+                }
+                if (t >= s.nt) continue;
+                const uint32_t i = job + (uint32_t)(kt - s.t0) * s.nt + t, buf = i & 1;
+                wait(kSFull + buf, (i >> 1) & 1);
+                tc_fence_after();
+                const uint32_t col_s = tb + my_lanes + kColS + kKeys * buf;
+                if (warp_live) {
+                    // masks are looked at where the tile is not full, or its last run passes the first row's position
+                    const int n_in = min(8, (stale ? s.r.n_stale : s.u.n_fp8) - (stale ? kt : kt - cut) * 8);
+                    bool masked = n_in < 8 || !ordinary;
+                    if (!masked && !stale) masked = (runs - s.r.n_fp8 + (kt - cut) * 8 + 7) * kPage + kPage - 1 > first_pos;
+                    int seen[8];                                 // tokens of run e that the row sees, from its first one
+                    if (masked) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            seen[e] = 0;
+                            if (e < n_in) {
+                                const int run = (stale ? kt : kt - cut) * 8 + e, pg = run / P.tiles, sub = run - pg * P.tiles;
+                                const int lp = list[stale ? pg : P.max_pages - 1 - pg].x;
+                                seen[e] = qpos - (lp * P.tiles + sub) * kPage + 1;
+                            }
+                        }
+                    }
+                    auto hide = [&](float (&x)[32], int c0) {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) {
+                            const int n = c0 + c;
+                            const bool out = stale ? token_of_row(n) >= seen[run_of_row(n)] : (n & 15) >= seen[n >> 4];
+                            if (out) x[c] = -CUDART_INF_F;
+                        }
+                    };
+                    float mx = -CUDART_INF_F;
+                    {
+                        float x[32];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            tmem_ld32(col_s + 32 * c, x);
+                            tmem_wait_ld();
+                            if (masked) hide(x, 32 * c);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) mx = fmaxf(mx, x[k]);
+                        }
+                        mx *= fac;
+                    }
+                    const bool raise = mx > ref + (kShift + kSlack);
+                    if (__any_sync(FULL, raise) || turn) {
+                        const float to = raise ? mx - kShift : ref;
+                        const float f = raise ? (ref == -CUDART_INF_F ? 0.f : fast_exp2(ref - to)) : 1.f;
+                        ref = to;
+                        sum *= f;
+                        if (n_done > 0) {
+                            const float fo = turn ? f * (__uint_as_float((uint32_t)(127 + P.ve) << 23) / P.v_scale) : f;
+                            wait(kPvDone + t, (done - 1) & 1);
+                            tc_fence_after();
+                            float x[32];
+#pragma unroll 1
+                            for (int c = 0; c < D / 32; ++c) {
+                                tmem_ld32(col_o + 32 * c, x);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) x[k] *= fo;
+                                tmem_st32(col_o + 32 * c, x);
+                            }
+                        }
+                    }
+                    const float base = ref == -CUDART_INF_F ? 0.f : ref;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        float x[32];
+                        uint32_t h2[16];
+                        tmem_ld32(col_s + 32 * c, x);
+                        tmem_wait_ld();
+                        if (masked) hide(x, 32 * c);
+                        float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const float a = fast_exp2(fmaf(x[2 * k], fac, -base)), d = fast_exp2(fmaf(x[2 * k + 1], fac, -base));
+                            s0 += a;
+                            s1 += d;
+                            h2[k] = pack_f16x2(a, d);
+                        }
+                        sum += s0 + s1;
+                        tmem_st16(col_s + 16 * c, h2);
+                    }
+                    tmem_wait_st();
+                }
+                tc_fence_before();
+                warp_arrive(kPFull + buf);
+                ++done;
+                ++n_done;
+            }
+            job += (uint32_t)(s.t1 - s.t0) * s.nt;
+            if (t < s.nt && warp_live) {
+                if (n_done > 0) {
+                    wait(kPvDone + t, (done - 1) & 1);
+                    tc_fence_after();
+                }
+                // accumulators are in units of the last tile's values
+                const float unit = s.t1 > cut ? P.v_scale : __uint_as_float((uint32_t)(127 + P.ve) << 23);
+                const bool none = sum == 0.f;
+                const float f = s.slot >= 0 ? unit : none ? 0.f : unit / sum;
+                const size_t orow = (size_t)(s.r.row0 + tok) * (P.hkv * P.group) + head;
+                const size_t prow = (size_t)max(s.slot, 0) * ROWS + my_row;
+#pragma unroll 1
+                for (int c = 0; c < D / 32; ++c) {
+                    float x[32];
+                    if (n_done > 0) {
+                        tmem_ld32(col_o + 32 * c, x);
+                        tmem_wait_ld();
+                    }
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        x[k] = none || n_done == 0 ? 0.f : x[k] * f;
+                        const unsigned long long note = nan_s[32 * c + k];
+                        if ((uint32_t)(note >> 32) == segments && kNoPos - (int)(uint32_t)note <= qpos) x[k] = CUDART_NAN_F;
+                    }
+                    if (!live) continue;
+                    if (s.slot >= 0) {
+                        float4* dst = reinterpret_cast<float4*>(P.part_o + prow * D + 32 * c);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) dst[k] = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+                    } else {
+                        uint4* dst = reinterpret_cast<uint4*>(P.out + orow * D + 32 * c);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            uint32_t o[4];
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                const __nv_bfloat162 p2 = __floats2bfloat162_rn(x[8 * k + 2 * q], x[8 * k + 2 * q + 1]);
+                                o[q] = *reinterpret_cast<const uint32_t*>(&p2);
+                            }
+                            dst[k] = make_uint4(o[0], o[1], o[2], o[3]);
+                        }
+                    }
+                }
+                if (live) {
+                    if (s.slot >= 0) P.part_ml[prow] = make_float2(ref, sum);
+                    else if (P.lse) P.lse[orow] = none ? -CUDART_INF_F : (ref + log2f(sum)) * 0.6931471805599453f;
+                }
+                tc_fence_before();
+            }
+            if (s.first_part && tid == 0) {
+                Merge m = {};
+                m.b = s.b; m.h = s.h; m.rt = s.rt; m.last = s.last_block; m.first_slot = s.slot;
+                P.merge[blockIdx.x] = m;
+            }
+            warp_arrive(kSegDone);
+        }
+    }
+    __syncthreads();
+    pdl_let_next_start();
+    tc_fence_after();
+    if (warp == G::MMA_WARP) tmem_dealloc(tb, 512);
+}
+
+// ---- merge ------------------------------------------------------------------------------------------
+// Rows of the units that several blocks share: a warp per row, parts in the order of their blocks.
+template <int D, int ROWS>
+__global__ void __launch_bounds__(256) chunk_merge_kernel(const Params P)
+{
+    pdl_begin();
+    const Merge m = P.merge[blockIdx.x];
+    if (m.b < 0) return;
+    const Request r = P.req[m.b];
+    const int lane = threadIdx.x & 31, in_unit = blockIdx.y * 8 + (threadIdx.x >> 5), row = m.rt * ROWS + in_unit;
+    if (row >= r.n_new * P.group) return;
+    const int parts = m.last - (int)blockIdx.x + 1;
+    auto slot = [&](int i) { return (size_t)(i == 0 ? m.first_slot : 2 * (blockIdx.x + i)) * ROWS + in_unit; };
+    float ref = -CUDART_INF_F;
+    for (int i = lane; i < parts; i += 32) ref = fmaxf(ref, P.part_ml[slot(i)].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor_sync(0xffffffffu, ref, o));
+    constexpr int N = D / 128;                                   // float4 of a lane
+    float4 acc[N];
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int i = 0; i < parts; ++i) {
+        const float2 ml = P.part_ml[slot(i)];
+        const float f = ml.x == -CUDART_INF_F ? (ml.y == 0.f ? 0.f : ml.y) : exp2f(ml.x - ref);   // a part with NaN scores only has no maximum
+        sum = fmaf(ml.y, f, sum);
+        const float4* src = reinterpret_cast<const float4*>(P.part_o + slot(i) * D);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float4 v = src[lane + 32 * k];
+            acc[k].x = fmaf(v.x, f, acc[k].x);
+            acc[k].y = fmaf(v.y, f, acc[k].y);
+            acc[k].z = fmaf(v.z, f, acc[k].z);
+            acc[k].w = fmaf(v.w, f, acc[k].w);
+        }
+    }
+    const int tok = row / P.group, head = m.h * P.group + row - tok * P.group;
+    const size_t orow = (size_t)(r.row0 + tok) * (P.hkv * P.group) + head;
+    const float f = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const __nv_bfloat162 a = __floats2bfloat162_rn(acc[k].x * f, acc[k].y * f), c = __floats2bfloat162_rn(acc[k].z * f, acc[k].w * f);
+        reinterpret_cast<uint2*>(P.out + orow * D)[lane + 32 * k] =
+            make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&c));
+    }
+    if (lane == 0 && P.lse) P.lse[orow] = sum == 0.f ? -CUDART_INF_F : (ref + log2f(sum)) * 0.6931471805599453f;
+}
+
+static size_t up(size_t x) { return (x + 255) / 256 * 256; }
+
+struct Layout { size_t req, merge, ml, o, list, bytes; };
+static Layout layout_of(int d, int B, int max_pages)
+{
+    const size_t rows = d == 128 ? Geo<128>::ROWS : Geo<256>::ROWS;
+    Layout l;
+    l.req = 0;
+    l.merge = up(l.req + sizeof(Request) * (size_t)B);
+    l.ml = up(l.merge + sizeof(Merge) * kMaxBlocks);
+    l.o = up(l.ml + sizeof(float2) * 2 * kMaxBlocks * rows);
+    l.list = up(l.o + sizeof(float) * 2 * kMaxBlocks * rows * d);
+    l.bytes = up(l.list + sizeof(int2) * (size_t)B * max_pages);
+    return l;
+}
+
+template <int D, int FMT>
+static int32_t launch(const Params& P, int sms, cudaStream_t s)
+{
+    using G = Geo<D>;
+    MKV_CUDA(cudaFuncSetAttribute(chunk_scan_kernel<D, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM));
+    const int blocks = sms < kMaxBlocks ? sms : kMaxBlocks;
+    MKV_CUDA(launch_pdl(chunk_plan_kernel<G::ROWS>, dim3(P.B), kPlanThreads, 0, 1, s, P));
+    MKV_CUDA(launch_pdl(chunk_scan_kernel<D, FMT>, dim3(blocks), G::THREADS, G::SMEM, 1, s, P));
+    MKV_CUDA(launch_pdl(chunk_merge_kernel<D, G::ROWS>, dim3(blocks, G::ROWS / 8), 256, 0, 1, s, P));
+    MKV_CUDA(cudaGetLastError());
+    return MKV_OK;
+}
+
+}  // namespace chunk
+
+size_t chunk_ws_bytes(int d, int B, int max_pages) { return chunk::layout_of(d, B, max_pages).bytes; }
+
+int32_t launch_chunk_attention(mkv_pool* p, const void* q, int64_t q_stride, int n_rows, const int32_t* starts, const int32_t* bt,
+                               const uint8_t* tags, const int32_t* lens, int B, int max_pages, float scale, void* out, float* lse,
+                               void* ws, cudaStream_t s)
+{
+    using namespace chunk;
+    Params P = {};
+    P.fp8 = p->fp8; P.tq3 = p->tq3;
+    P.fp8_pages = p->cfg.fp8_pages; P.tq3_pages = p->cfg.tq3_pages;
+    P.hkv = p->hkv; P.group = p->group; P.tiles = p->tiles;
+    P.sigma = p->sigma;
+    P.sc2 = (scale < 0.f ? -scale : scale) * kLog2e;
+    P.negative = scale < 0.f;
+    P.k_scale = p->cfg.k_scale; P.v_scale = p->cfg.v_scale;
+    // Demote writes numbers of at most 448 times the pool's scales: units of their size keep fp16 from overflow
+    auto unit = [](float x) {
+        int e;
+        frexpf(x, &e);
+        return e - 1 < -14 ? -14 : e - 1 > 14 ? 14 : e - 1;
+    };
+    P.ke = unit(P.k_scale); P.ve = unit(P.v_scale);
+    P.q = static_cast<const __nv_bfloat16*>(q);
+    P.q_stride = q_stride;
+    P.n_rows = n_rows;
+    P.starts = starts; P.bt = bt; P.lens = lens; P.tags = tags;
+    P.B = B; P.max_pages = max_pages;
+    P.out = static_cast<__nv_bfloat16*>(out);
+    P.lse = lse;
+    const Layout l = layout_of(p->d, B, max_pages);
+    uint8_t* w = static_cast<uint8_t*>(ws);
+    P.req = reinterpret_cast<Request*>(w + l.req);
+    P.merge = reinterpret_cast<Merge*>(w + l.merge);
+    P.part_ml = reinterpret_cast<float2*>(w + l.ml);
+    P.part_o = reinterpret_cast<float*>(w + l.o);
+    P.list = reinterpret_cast<int2*>(w + l.list);
+    P.status = p->status_dev;
+    P.wait_ns = p->wait_ns;
+    const int sms = p->dev.sm_count;
+    if (p->d == 128) return p->fmt == 2 ? launch<128, 2>(P, sms, s) : launch<128, 1>(P, sms, s);
+    return p->fmt == 2 ? launch<256, 2>(P, sms, s) : launch<256, 1>(P, sms, s);
+}
+
+}  // namespace mkv

@@ -34,10 +34,10 @@
 
 #include "decode_cut.cuh"
 #include "mkv_internal.cuh"
+#include "tensor_ptx.cuh"
 
 namespace mkv {
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRescaleSlack = 8.0f;                        // the running maximum is only raised when exceeded by 2^8
 constexpr unsigned long long kDefaultWaitNs = 20000000ull;   // 20 ms: far beyond any copy that is going to arrive
@@ -88,224 +88,6 @@ struct LayerSet {
     int n;
     DecodeParams layer[MAXL];
 };
-
-// ------------------------------------------------------------------------------------------------
-// small PTX wrappers
-// ------------------------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t s)
-{
-    uint32_t r;
-    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(s));
-    return r;
-}
-
-// (a & b) | c in one LOP3
-__device__ __forceinline__ uint32_t lop3_and_or(uint32_t a, uint32_t b, uint32_t c)
-{
-    uint32_t r;
-    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
-    return r;
-}
-
-__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
-{
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-// same product with a zero accumulator: d = A B
-__device__ __forceinline__ void mma16816_zero(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
-{
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
-}
-
-// D += A B with signed 8-bit integer operands and 32-bit integer accumulators: A 16 x 32 (row-major fragment),
-// B 32 x 8.  (Measured on B200: this legacy integer MMA is one native instruction at the rate of the fp16
-// m16n8k16 one, i.e. twice its products per instruction; the e4m3 form of mma.sync is expanded by the compiler
-// into conversions and fp16 MMAs and is slower than the fp16 path it was meant to replace.)
-__device__ __forceinline__ void mma16832_s8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
-{
-    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
-// the same product with a zero accumulator
-__device__ __forceinline__ void mma16832_s8_zero(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
-{
-    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-                 : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "r"(0));
-}
-
-__device__ __forceinline__ uint32_t lds32(uint32_t addr)
-{
-    uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr));
-    return v;
-}
-
-__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x)
-{
-    uint32_t r;
-    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
-    return r;
-}
-
-__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
-{
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-
-__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint16_t v)
-{
-    uint32_t r;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(v));
-    return r;
-}
-
-__device__ __forceinline__ float fast_exp2(float x)
-{
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-
-__device__ __forceinline__ uint32_t hfma2_u32(uint32_t a, uint32_t b, uint32_t c)
-{
-    uint32_t r;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
-    return r;
-}
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
-}
-
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-
-__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-
-__device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-
-// Arrival on a row's ticket: what this block has stored (before a block barrier) is released, what the others have is acquired
-__device__ __forceinline__ uint32_t ticket_add(uint32_t* p, uint32_t v)
-{
-    uint32_t old;
-    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], %2;" : "=r"(old) : "l"(p), "r"(v) : "memory");
-    return old;
-}
-
-__device__ __forceinline__ uint32_t ticket_or(uint32_t* p, uint32_t v)
-{
-    uint32_t old;
-    asm volatile("atom.or.acq_rel.gpu.global.b32 %0, [%1], %2;" : "=r"(old) : "l"(p), "r"(v) : "memory");
-    return old;
-}
-
-// bulk asynchronous copy global -> this block's shared memory, completion counted on an mbarrier
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
-
-__device__ __forceinline__ uint4 lds128(uint32_t addr)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
-    return v;
-}
-
-__device__ __forceinline__ uint2 lds64(uint32_t addr)
-{
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
-    return v;
-}
-
-__device__ __forceinline__ uint16_t lds16(uint32_t addr)
-{
-    uint16_t v;
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr));
-    return v;
-}
-
-// ------------------------------------------------------------------------------------------------
-// TQ3 unpack
-// ------------------------------------------------------------------------------------------------
-// Four 3-bit key codes in the four low nibbles of `sel` (bit 3 of each nibble clear) -> two half2
-// registers holding the signed fp16 codebook levels.  The two byte tables hold the high and the low
-// bytes of {+C0,+C1,+C2,+C3,-C0,-C1,-C2,-C3} = fp16 {33D8, 3A0C, 3D60, 404E | sign}.
-__device__ __forceinline__ void key_lut4(uint32_t sel, uint32_t& r0, uint32_t& r1)
-{
-    const uint32_t hi = prmt(0x403D3A33u, 0xC0BDBAB3u, sel);
-    const uint32_t lo = prmt(0x4E600CD8u, 0x4E600CD8u, sel);
-    r0 = prmt(lo, hi, 0x5140u);
-    r1 = prmt(lo, hi, 0x7362u);
-}
-
-// Two 3-bit value codes sitting at bit POS of each 16-bit half of x -> half2 of the integer codes.
-// (x & mask) | 0x6400 is the fp16 number 1024 + code * 2^POS; one FMA recovers the code exactly.
-// (The masked bits alone are the exact operand code * 2^(POS - 24), a subnormal, and save the FMA: 2 x 59,008 tokens in
-// 16 layers 554 -> 592 us with it.  But the tensor core aligns the products of an MMA by the exponents of their factors,
-// and a subnormal has the exponent of the first binade: every bit that a code stands below bit 10 is a bit less of the
-// sum.  Rows of 30,000 equally weighted tokens came out 3 to 4 times as far from the fp64 result, 3e-6 to 5e-6 against
-// 1e-6, with codes at bits 5 to 8, and 100 times with codes left where they are.)
-template <int POS>
-__device__ __forceinline__ uint32_t value_code(uint32_t x)
-{
-    constexpr uint32_t mask = 0x00070007u << POS;
-    const uint32_t u = lop3_and_or(x, mask, 0x64006400u);
-    // 2^-POS and -1024 * 2^-POS as fp16 pairs (exponent arithmetic on 1.0 = 0x3C00, -1024 = 0xE400)
-    constexpr uint32_t mul = (0x3C00u - (POS << 10)) * 0x00010001u;
-    constexpr uint32_t add = (0xE400u - (POS << 10)) * 0x00010001u;
-    return hfma2_u32(u, mul, add);
-}
-
-// A operands of the four channel blocks of a word triple
-template <int BLOCK>
-__device__ __forceinline__ void value_operands(uint32_t (&a)[4], uint32_t W0, uint32_t W1, uint32_t W2, uint32_t X)
-{
-    if constexpr (BLOCK == 0) {          // X = bytes of W0, W1 between the two
-        a[0] = value_code<0>(W0); a[1] = value_code<3>(W0); a[2] = value_code<6>(W0); a[3] = value_code<1>(X);
-    } else if constexpr (BLOCK == 1) {
-        a[0] = value_code<4>(X); a[1] = value_code<7>(X); a[2] = value_code<2>(W1); a[3] = value_code<5>(W1);
-    } else if constexpr (BLOCK == 2) {   // X = bytes of W1, W2
-        a[0] = value_code<0>(X); a[1] = value_code<3>(X); a[2] = value_code<6>(X); a[3] = value_code<1>(W2);
-    } else {
-        const uint32_t X2 = W2 >> 8;
-        a[0] = value_code<4>(W2); a[1] = value_code<7>(W2); a[2] = value_code<2>(X2); a[3] = value_code<5>(X2);
-    }
-}
-
-__device__ __forceinline__ float2 half2_to_float2(uint32_t x)
-{
-    return __half22float2(*reinterpret_cast<const __half2*>(&x));
-}
 
 // acc[channel rows g, g+8][heads] += scale_row * t + zero_row * psum_head
 __device__ __forceinline__ void affine_accumulate(float (&acc)[4], const float (&t)[4], uint32_t sc_pair, uint32_t zp_pair,

@@ -182,6 +182,10 @@ int32_t launch_append_layers(mkv_pool* const* pools, const void* const* k, const
                              int n_tokens, int n_layers, cudaStream_t s);
 int32_t launch_page_score(const float* mass, const int32_t* lens, int B, int hq, int max_pages, uint64_t head_mask,
                           float beta, float* score, int page_tokens, cudaStream_t s);
+int32_t launch_chunk_attention(mkv_pool* p, const void* q, int64_t q_stride, int n_rows, const int32_t* starts, const int32_t* bt,
+                               const uint8_t* tags, const int32_t* lens, int B, int max_pages, float scale, void* out, float* lse,
+                               void* ws, cudaStream_t s);
+size_t chunk_ws_bytes(int d, int B, int max_pages);
 constexpr int kMaxCtas = 512;        // upper bound of the decode scan's persistent grid (sizes workspace and tickets)
 int decode_tensor_partial_floats(int d);
 void set_last_error(const char* msg);

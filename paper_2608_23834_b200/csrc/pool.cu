@@ -413,6 +413,33 @@ int32_t mkv_decode_attention_scored(mkv_pool* pool, const void* q, const int32_t
                                    page_mass, (cudaStream_t)stream);
 }
 
+int32_t mkv_chunk_workspace_bytes(const mkv_pool_config* cfg, int32_t max_batch, int32_t max_pages, size_t* bytes)
+{
+    int32_t rc = check_cfg(cfg);
+    if (rc) return rc;
+    if (!bytes || max_batch < 1 || max_pages < 1) return MKV_E_INVALID;
+    *bytes = chunk_ws_bytes(cfg->head_dim, max_batch, max_pages);
+    return MKV_OK;
+}
+
+int32_t mkv_chunk_attention(mkv_pool* pool, const void* q, int64_t q_stride, int32_t n_rows, const int32_t* starts,
+                            const int32_t* bt, const uint8_t* tags, const int32_t* lens, int32_t B, int32_t max_pages,
+                            float scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream)
+{
+    if (!pool || !pool->fp8 || B < 0 || max_pages < 0 || n_rows < 0) return MKV_E_INVALID;
+    if (B == 0 || n_rows == 0) return MKV_OK;
+    if (max_pages > 0 && (!bt || !tags)) return MKV_E_INVALID;
+    if (!q || !starts || !lens || !out || !ws) return MKV_E_INVALID;
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(ws, 256) || !aligned(bt, 4) || !aligned(lens, 4) || !aligned(starts, 4) ||
+        !aligned(lse, 4))
+        return MKV_E_INVALID;
+    if (q_stride < (int64_t)pool->hq * pool->d || q_stride % 8) return MKV_E_INVALID;
+    if (!(scale - scale == 0.f)) return MKV_E_INVALID;              // infinite, or not a number
+    if (ws_bytes < chunk_ws_bytes(pool->d, B, max_pages)) return MKV_E_INVALID;
+    return launch_chunk_attention(pool, q, q_stride, n_rows, starts, bt, tags, lens, B, max_pages, scale, out, lse, ws,
+                                  (cudaStream_t)stream);
+}
+
 int32_t mkv_page_score_update_paged(const float* page_mass, const int32_t* lens, int32_t B, int32_t n_q_heads,
                                     int32_t max_pages, int32_t page_size, uint64_t head_mask, float beta, float* score,
                                     void* stream)

@@ -6,6 +6,7 @@
 // returns 0 (enqueued), a negative mkv_status, or kCheck when an argument is not what the call takes; nothing has
 // been enqueued then and the Python caller goes through its own checks, which say what is wrong.
 #include <Python.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -18,7 +19,7 @@ constexpr long kCheck = 1;
 // what the checks of a call need of its pool (held by the Python Pool as a capsule)
 struct PoolRef {
     mkv_pool* pool;
-    int hkv, hq, d;
+    int hkv, hq, d, device;
 };
 const char* kCapsule = "mkv.pool_ref";
 PyObject *s_workspace, *s_ref, *s_cuda_stream, *s_ws_bytes;
@@ -27,8 +28,8 @@ void free_ref(PyObject* capsule) { delete static_cast<PoolRef*>(PyCapsule_GetPoi
 
 PyObject* pool_ref(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
-    if (n != 4) {
-        PyErr_SetString(PyExc_TypeError, "pool_ref(handle, kv_heads, q_heads, head_dim)");
+    if (n != 5) {
+        PyErr_SetString(PyExc_TypeError, "pool_ref(handle, kv_heads, q_heads, head_dim, device)");
         return nullptr;
     }
     auto* r = new PoolRef;
@@ -36,6 +37,7 @@ PyObject* pool_ref(PyObject*, PyObject* const* a, Py_ssize_t n)
     r->hkv = (int)PyLong_AsLong(a[1]);
     r->hq = (int)PyLong_AsLong(a[2]);
     r->d = (int)PyLong_AsLong(a[3]);
+    r->device = (int)PyLong_AsLong(a[4]);
     if (PyErr_Occurred()) {
         delete r;
         return nullptr;
@@ -202,6 +204,65 @@ PyObject* decode_scored(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
+// bf16 [n][heads][d] whose tokens may lie apart; *stride: elements from a token to the next
+bool is_rows(const at::Tensor* t, int64_t n, int64_t heads, int64_t d, int64_t* stride)
+{
+    if (!is(t, at::kBFloat16) || t->dim() != 3 || !shape3(t, n, heads, d)) return false;
+    if (t->stride(2) != 1 || (heads > 1 && t->stride(1) != d)) return false;
+    *stride = n > 1 ? t->stride(0) : heads * d;
+    return *stride >= heads * d && *stride % 8 == 0;
+}
+
+// None or a dense fp32 tensor of [n][heads]
+bool optional_lse(PyObject* o, int64_t n, int64_t heads, void** ptr)
+{
+    *ptr = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor* t = tensor(o);
+    if (!is_dense(t, at::kFloat) || !same_shape2(t, n, heads)) return false;
+    *ptr = t->data_ptr();
+    return true;
+}
+
+// chunk_attention(ref, q, q_starts, block_table, tier_tag, seq_lens, scale, out, lse, workspace, stream)
+PyObject* chunk_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    const PoolRef* r = n == 11 ? ref_of(a[0]) : nullptr;
+    if (!r) return result(kCheck);
+    const at::Tensor *q = tensor(a[1]), *starts = tensor(a[2]), *bt = tensor(a[3]), *tags = tensor(a[4]), *lens = tensor(a[5]),
+                     *out = tensor(a[7]), *ws = tensor(a[9]);
+    int64_t stride;
+    void *lse, *s;
+    if (!q || q->dim() != 3 || !is_rows(q, q->size(0), r->hq, r->d, &stride) || !is_dense(lens, at::kInt)) return result(kCheck);
+    const int64_t B = lens->numel(), rows = q->size(0);
+    if (!is_dense(starts, at::kInt) || starts->numel() != B + 1 || !is_dense(bt, at::kInt) || bt->dim() != 2 || bt->size(0) != B ||
+        !is_dense(tags, at::kByte) || !same_shape2(tags, B, bt->size(1)) || !is_dense(out, at::kBFloat16) || out->dim() != 3 ||
+        !shape3(out, rows, r->hq, r->d) || !is_dense(ws, at::kByte) || !optional_lse(a[8], rows, r->hq, &lse))
+        return result(kCheck);
+    const c10::Device dev(c10::kCUDA, (c10::DeviceIndex)r->device);
+    if (q->device() != dev || starts->device() != dev || bt->device() != dev || tags->device() != dev || lens->device() != dev ||
+        out->device() != dev || ws->device() != dev || (lse && tensor(a[8])->device() != dev))
+        return result(kCheck);
+    const float scale = (float)PyFloat_AsDouble(a[6]);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        return result(kCheck);
+    }
+    const c10::cuda::CUDAGuard guard(dev);
+    if (!stream_of(a[10], &s)) return result(kCheck);
+    const void* qp = q->data_ptr();
+    const auto *sp = static_cast<const int32_t*>(starts->data_ptr()), *bp = static_cast<const int32_t*>(bt->data_ptr()),
+               *lp = static_cast<const int32_t*>(lens->data_ptr());
+    const auto* tp = static_cast<const uint8_t*>(tags->data_ptr());
+    void *op = out->data_ptr(), *wp = ws->data_ptr();
+    const size_t ws_bytes = (size_t)ws->numel();
+    const int width = (int)bt->size(1);
+    return enqueue([=] {
+        return mkv_chunk_attention(r->pool, qp, stride, (int)rows, sp, bp, tp, lp, (int)B, width, scale, op,
+                                   static_cast<float*>(lse), wp, ws_bytes, s);
+    });
+}
+
 // A Python sequence of at least n items; PySequence_Fast objects are released on destruction.
 struct Items {
     PyObject* fast;
@@ -336,7 +397,8 @@ PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n)
 PyMethodDef methods[] = {
     FAST("pool_ref", pool_ref), FAST("append", append), FAST("demote", convert<mkv_demote>), FAST("promote", convert<mkv_promote>),
     FAST("decode", decode), FAST("decode_scored", decode_scored), FAST("decode_layers", decode_layers),
-    FAST("append_layers", append_layers), FAST("score_update", score_update), {nullptr, nullptr, 0, nullptr}};
+    FAST("append_layers", append_layers), FAST("score_update", score_update),
+    FAST("chunk_attention", chunk_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mkv_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
