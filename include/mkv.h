@@ -183,6 +183,35 @@ const char* mkv_last_cuda_error(void);
 int32_t mkv_append(mkv_pool* pool, const void* k_dev, const void* v_dev, const int32_t* slot_mapping_dev,
                    int32_t n_tokens, void* stream);
 
+/* Append with the rotation of positions on the way: the queries, keys and values of n tokens as a projection leaves them.
+ * Queries are turned and written to q_out (bf16); keys are turned and stored as e4m3, from fp32 in one rounding; values are
+ * stored as by mkv_append.  Pair j of a head, the dims (j, j + rotary_dim / 2) or, interleaved, (2 j, 2 j + 1), is turned by
+ * the angle inv_freq[j] * positions[axis[j]][token]; the dims from rotary_dim on pass as they are.  One launch.
+ *   mkv_rotary   what a model keeps per rotation:
+ *     turns_dev    device, uint64 [rotary_dim / 2]: inv_freq / (2 pi) in units of 2^-64 turns (mkv_rotary_turns, a host
+ *                  call): angles stay exact to 2^-32 of a turn for every int32 position, negative ones included
+ *     axis_dev     device, uint8 [rotary_dim / 2]: axis of every pair (time, height, width, ...), below n_axes (read as
+ *                  n_axes - 1 beyond); NULL with one axis
+ *     rotary_dim   multiple of 16, at most d
+ *     mscale       finite; turned dims are multiplied by it (a long-context attention factor), 1 otherwise
+ *   q, k, v      device, bf16 [n][heads][d], heads dense, *_stride elements from a token to the next (a multiple of 8), so
+ *                that slices of one fused projection are taken as they stand; q may be NULL (with q_out), k may be NULL (with v)
+ *   slot_mapping device, int32 [n], as mkv_append: a negative slot stores nothing (its query is turned all the same); two
+ *                tokens with the same slot: which of them stays is not defined
+ *   positions    device, int32 [n_axes][n]
+ *   q_out        device, bf16, out_stride elements from a token to the next; may be q itself with q's stride, and must
+ *                not overlap it otherwise */
+typedef struct {
+    const uint64_t* turns_dev;
+    const uint8_t* axis_dev;
+    int32_t rotary_dim, n_axes, interleaved;
+    float mscale;
+} mkv_rotary;
+int32_t mkv_rotary_turns(const double* inv_freq, int32_t n, uint64_t* turns);
+int32_t mkv_append_rotary(mkv_pool* pool, const void* q_dev, int64_t q_stride, const void* k_dev, int64_t k_stride,
+                          const void* v_dev, int64_t v_stride, const int32_t* slot_mapping_dev, const int32_t* positions_dev,
+                          int32_t n, const mkv_rotary* rotary, void* q_out_dev, int64_t out_stride, void* stream);
+
 /* Demote / Retier(p, TQ3) (Algorithm 1 step 2; Section 4, "normalize-rotate-pack"): encode
  * n_pages full FP8 pages (all KV heads) into TQ3 pages, then publish.
  *   src_fp8_ids, dst_tq3_ids   device, int32 [n_pages]

@@ -36,7 +36,7 @@ EXPORTS = [
     "mkv_decode_attention_static", "mkv_promote", "mkv_seq_promote",
     "mkv_decode_attention_scored", "mkv_page_score_update", "mkv_page_score_update_paged",
     "mkv_decode_attention_layers", "mkv_append_layers", "mkv_pool_set_wait_limit_ns", "mkv_seq_release",
-    "mkv_chunk_workspace_bytes", "mkv_chunk_attention",
+    "mkv_chunk_workspace_bytes", "mkv_chunk_attention", "mkv_rotary_turns", "mkv_append_rotary",
 ]
 MAX_LAYERS_PER_CALL = 32
 
@@ -69,6 +69,11 @@ class LayerCall(C.Structure):
 
 class LayerAppend(C.Structure):
     _fields_ = [("pool", C.c_void_p), ("k_dev", C.c_void_p), ("v_dev", C.c_void_p)]
+
+
+class RotaryStruct(C.Structure):
+    _fields_ = [("turns_dev", C.c_void_p), ("axis_dev", C.c_void_p), ("rotary_dim", C.c_int32), ("n_axes", C.c_int32),
+                ("interleaved", C.c_int32), ("mscale", C.c_float)]
 
 
 def lib():
@@ -111,6 +116,9 @@ def lib():
             "mkv_decode_attention_layers": [C.POINTER(LayerCall), C.c_int32, vp, C.c_int32, C.c_int32, C.c_float,
                                             C.c_size_t, vp],
             "mkv_append_layers": [C.POINTER(LayerAppend), C.c_int32, vp, C.c_int32, vp],
+            "mkv_rotary_turns": [vp, C.c_int32, vp],
+            "mkv_append_rotary": [vp, vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, vp, vp, C.c_int32, C.POINTER(RotaryStruct), vp,
+                                  C.c_int64, vp],
             "mkv_chunk_workspace_bytes": [cfgp, C.c_int32, C.c_int32, szp],
             "mkv_chunk_attention": [vp, vp, C.c_int64, C.c_int32, vp, vp, vp, vp, C.c_int32, C.c_int32, C.c_float, vp, f32p,
                                     vp, C.c_size_t, vp],
@@ -186,6 +194,38 @@ def mkv_decode_workspace_bytes(cfg: PoolConfig, max_batch: int) -> int:
     n = C.c_size_t()
     _check(lib().mkv_decode_workspace_bytes(C.byref(cfg), max_batch, C.byref(n)), "mkv_decode_workspace_bytes")
     return n.value
+
+
+def mkv_rotary_turns(inv_freq) -> np.ndarray:
+    f = np.ascontiguousarray(inv_freq, np.float64)
+    turns = np.zeros(f.shape, np.uint64)
+    _check(lib().mkv_rotary_turns(C.c_void_p(f.ctypes.data), f.size, C.c_void_p(turns.ctypes.data)), "mkv_rotary_turns")
+    return turns
+
+
+class Rotary:
+    """The rotation of a model's queries and keys by their positions (mkv_rotary), kept for all its calls on a device.
+
+    inv_freq: radians per position of every pair of dims; 2 * len(inv_freq) dims of a head turn (a multiple of 16).
+    axes: axis of every pair where positions have several (time, height, width); None: one axis.
+    interleaved: pairs (2 j, 2 j + 1) instead of (j, j + len(inv_freq)).  mscale: factor of the turned dims."""
+
+    def __init__(self, inv_freq, axes=None, interleaved=False, mscale=1.0, device="cuda:0"):
+        inv_freq = np.ascontiguousarray(inv_freq.double().cpu().numpy() if isinstance(inv_freq, torch.Tensor) else inv_freq, np.float64)
+        assert inv_freq.ndim == 1 and inv_freq.size >= 8 and inv_freq.size % 8 == 0, "inv_freq: a multiple of 8 pairs"
+        self.rotary_dim, self.interleaved, self.mscale = 2 * inv_freq.size, bool(interleaved), float(mscale)
+        assert np.isfinite(self.mscale), "mscale: finite"
+        turns = mkv_rotary_turns(inv_freq)
+        self.axis, self.n_axes = None, 1
+        if axes is not None:
+            axes = np.asarray(axes.cpu() if isinstance(axes, torch.Tensor) else axes)
+            assert axes.shape == inv_freq.shape and axes.min() >= 0 and axes.max() < 256, "axes: one axis per pair"
+            self.n_axes = int(axes.max()) + 1
+            self.axis = torch.from_numpy(axes.astype(np.uint8)).to(device)
+        self.turns = torch.from_numpy(turns.view(np.int64)).to(device)
+        self.struct = RotaryStruct(self.turns.data_ptr(), None if self.axis is None else self.axis.data_ptr(), self.rotary_dim, self.n_axes,
+                                   int(self.interleaved), self.mscale)
+        self._ref = C.addressof(self.struct)
 
 
 class Pool:
@@ -283,6 +323,40 @@ class Pool:
         assert k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and slot_mapping.dtype == torch.int32
         assert k.is_contiguous() and v.is_contiguous() and k.shape == v.shape and k.shape[1:] == (self.hkv, self.d)
         _check(lib().mkv_append(self.handle, _ptr(k), _ptr(v), _ptr(slot_mapping), k.shape[0], _stream(stream)), "mkv_append")
+
+    def append_rotary(self, q, k, v, slot_mapping, positions, rotary: Rotary, q_out=None, stream=None):
+        """mkv_append_rotary: Append of k and v with q and k turned by their positions (int32 [tokens], or [axes][tokens]) on
+        the way; returns the turned queries (q_out; q itself for a turn in place).  The tokens of q, k and v may lie apart
+        (slices of a fused projection).  q may be None (keys and values only), k and v too (queries only)."""
+        if q_out is not None and _native_rc(_native.append_rotary(self._ref, q, k, v, slot_mapping, positions, rotary._ref,
+                                                                  rotary.turns, rotary.n_axes, q_out, stream), "mkv_append_rotary"):
+            return q_out
+        assert (k is None) == (v is None) and (q is not None or k is not None), "q, or k and v, or all"
+        n = (q if q is not None else k).shape[0]
+        tensors = [positions, rotary.turns]
+        if q is not None:
+            self._check_rows(q, n, self.hq, "q")
+            if q_out is None:
+                q_out = torch.empty((n, self.hq, self.d), dtype=torch.bfloat16, device=q.device)
+            self._check_rows(q_out, n, self.hq, "q_out")
+            tensors += [q, q_out]
+        else:
+            assert q_out is None, "q_out without q"
+        if k is not None:
+            self._check_rows(k, n, self.hkv, "k")
+            self._check_rows(v, n, self.hkv, "v")
+            assert slot_mapping.dtype == torch.int32 and slot_mapping.is_contiguous() and slot_mapping.numel() == n
+            tensors += [k, v, slot_mapping]
+        assert positions.dtype == torch.int32 and positions.is_contiguous(), "positions: dense int32"
+        assert positions.shape == (rotary.n_axes, n) or (rotary.n_axes == 1 and positions.shape == (n,)), "positions: [axes][tokens]"
+        assert rotary.rotary_dim <= self.d, "rotary_dim: at most head_dim"
+        assert all(t.device == self.fp8_arena.device for t in tensors), "every tensor is on the pool's device"
+        step = lambda t, heads: 0 if t is None else t.stride(0) if n > 1 else heads * self.d
+        with torch.cuda.device(self.fp8_arena.device):
+            _check(lib().mkv_append_rotary(self.handle, _ptr(q), step(q, self.hq), _ptr(k), step(k, self.hkv), _ptr(v), step(v, self.hkv),
+                                           _ptr(slot_mapping) if k is not None else None, _ptr(positions), n, C.byref(rotary.struct),
+                                           _ptr(q_out), step(q_out, self.hq), _stream(stream)), "mkv_append_rotary")
+        return q_out
 
     def demote(self, src_ids: torch.Tensor, dst_ids: torch.Tensor, block_table=None, tier_tag=None, entry_index=None,
                stream=None) -> None:

@@ -81,6 +81,65 @@ __device__ __forceinline__ uint2 bf16x8_to_e4m3x8(uint4 in, float inv_scale)
     return make_uint2(q[0] | (q[1] << 16), q[2] | (q[3] << 16));
 }
 
+// The runs that start in the window of 16 tokens from t0 on (first warp of a block): slots of this window and the next,
+// the token whose run fills a tile of the store (at most one starts in a window; -1: none), and the tokens of the other runs.
+struct RunWindow {
+    int32_t slot[2 * kPage];
+    int32_t rest[2 * kPage];
+    int full, n_rest;
+};
+
+__device__ __forceinline__ void find_runs(RunWindow& w, const int32_t* slots, int n, int t0, int tiles, int fp8_pages, int tid)
+{
+    const int sl = t0 + tid < n ? slots[t0 + tid] : -1;
+    const int before = tid == 0 && t0 > 0 ? slots[t0 - 1] : -2;
+    w.slot[tid] = sl;
+    const int up = __shfl_up_sync(0xffffffffu, sl, 1);
+    const int prev = tid == 0 ? before : up;
+    __syncwarp();
+    int len = 0;
+    if (tid < kPage && sl >= 0 && ((sl & 15) == 0 || prev != sl - 1)) {
+        len = 1;
+        while (len < kPage - (sl & 15) && w.slot[tid + len] == sl + len) ++len;
+    }
+    const bool full = len == kPage && (sl >> 4) / tiles < fp8_pages;
+    const uint32_t m = __ballot_sync(0xffffffffu, full);
+    if (full) len = 0;
+    int end = len;                                   // running count of those tokens
+#pragma unroll
+    for (int o = 1; o < kPage; o <<= 1) {
+        const int before_me = __shfl_up_sync(0xffffffffu, end, o);
+        if (tid >= o) end += before_me;
+    }
+    for (int j = 0; j < len; ++j) w.rest[end - len + j] = tid + j;
+    if (tid == 0) w.full = m ? __ffs(m) - 1 : -1;
+    if (tid == kPage - 1) w.n_rest = end;
+}
+
+// Values of a whole tile, token rows of D + 4 bytes in shared memory -> channel-major record.  Thread c4 owns channels
+// 4 c4 .. 4 c4 + 3: 16 words (one per token) -> 4 x 16 bytes.
+template <int D, int THREADS>
+__device__ __forceinline__ void store_value_tile(uint8_t* __restrict__ rec, const uint8_t* vt, int tid)
+{
+    constexpr int VROW = D + 4;
+    for (int c4 = tid; c4 < D / 4; c4 += THREADS) {
+        uint32_t w[kPage];
+#pragma unroll
+        for (int t = 0; t < kPage; ++t) w[t] = *reinterpret_cast<const uint32_t*>(vt + t * VROW + 4 * c4);
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch) {
+            uint32_t o[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t lo = __byte_perm(w[4 * q], w[4 * q + 1], 0x0040 + 0x0011 * ch);   // bytes ch of t, t+1
+                const uint32_t hi = __byte_perm(w[4 * q + 2], w[4 * q + 3], 0x0040 + 0x0011 * ch);
+                o[q] = __byte_perm(lo, hi, 0x5410);
+            }
+            *reinterpret_cast<uint4*>(rec + 16 * D + (4 * c4 + ch) * kPage) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+    }
+}
+
 // Prefill-sized calls: one block per (window of 16 consecutive input tokens, KV head).  The block takes the runs
 // that START in its window, a run being consecutive tokens that go to consecutive positions of one 16-token tile;
 // such a run may reach up to 15 tokens into the next window.  A chunk of a request that starts anywhere inside a
@@ -99,38 +158,13 @@ __global__ void __launch_bounds__(128) append_run_kernel(uint8_t* __restrict__ f
 {
     constexpr int VROW = D + 4;                      // padded token row of the transposition tile
     __shared__ __align__(16) uint8_t vt[kPage * VROW];
-    __shared__ int32_t slot_s[2 * kPage];            // slots of this window and the next
-    __shared__ int32_t rest_s[2 * kPage];            // tokens of the other runs that start in the window
-    __shared__ int full_s, n_rest_s;                 // token whose run fills a tile (at most one starts in a window), or -1
+    __shared__ RunWindow win;
+    const int32_t *slot_s = win.slot, *rest_s = win.rest;
     pdl_begin();
     const int t0 = blockIdx.x * kPage, h = blockIdx.y, tid = threadIdx.x;
-    if (tid < 32) {
-        const int sl = t0 + tid < n ? slots[t0 + tid] : -1;
-        const int before = tid == 0 && t0 > 0 ? slots[t0 - 1] : -2;
-        slot_s[tid] = sl;
-        const int up = __shfl_up_sync(0xffffffffu, sl, 1);
-        const int prev = tid == 0 ? before : up;
-        __syncwarp();
-        int len = 0;
-        if (tid < kPage && sl >= 0 && ((sl & 15) == 0 || prev != sl - 1)) {
-            len = 1;
-            while (len < kPage - (sl & 15) && slot_s[tid + len] == sl + len) ++len;
-        }
-        const bool full = len == kPage && (sl >> 4) / tiles < fp8_pages;
-        const uint32_t m = __ballot_sync(0xffffffffu, full);
-        if (full) len = 0;
-        int end = len;                               // running count of those tokens
-#pragma unroll
-        for (int o = 1; o < kPage; o <<= 1) {
-            const int before_me = __shfl_up_sync(0xffffffffu, end, o);
-            if (tid >= o) end += before_me;
-        }
-        for (int j = 0; j < len; ++j) rest_s[end - len + j] = tid + j;
-        if (tid == 0) full_s = m ? __ffs(m) - 1 : -1;
-        if (tid == kPage - 1) n_rest_s = end;
-    }
+    if (tid < 32) find_runs(win, slots, n, t0, tiles, fp8_pages, tid);
     __syncthreads();
-    const int full = full_s;
+    const int full = win.full;
     if (full >= 0) {
         const int gt = slot_s[full] >> 4, page = gt / tiles;
         uint8_t* rec = fp8 + (((size_t)page * hkv + h) * tiles + (gt - page * tiles)) * fp8_record_bytes(D);
@@ -153,26 +187,10 @@ __global__ void __launch_bounds__(128) append_run_kernel(uint8_t* __restrict__ f
             *reinterpret_cast<uint32_t*>(vt + t * VROW + 8 * c8 + 4) = vq.y;
         }
         __syncthreads();
-        // thread c4 owns channels 4 c4 .. 4 c4 + 3: 16 words (one per token) -> 4 x 16 bytes
-        for (int c4 = tid; c4 < D / 4; c4 += 128) {
-            uint32_t w[kPage];
-#pragma unroll
-            for (int t = 0; t < kPage; ++t) w[t] = *reinterpret_cast<const uint32_t*>(vt + t * VROW + 4 * c4);
-#pragma unroll
-            for (int ch = 0; ch < 4; ++ch) {
-                uint32_t o[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t lo = __byte_perm(w[4 * q], w[4 * q + 1], 0x0040 + 0x0011 * ch);   // bytes ch of t, t+1
-                    const uint32_t hi = __byte_perm(w[4 * q + 2], w[4 * q + 3], 0x0040 + 0x0011 * ch);
-                    o[q] = __byte_perm(lo, hi, 0x5410);
-                }
-                *reinterpret_cast<uint4*>(rec + 16 * D + (4 * c4 + ch) * kPage) = make_uint4(o[0], o[1], o[2], o[3]);
-            }
-        }
+        store_value_tile<D, 128>(rec, vt, tid);
     }
     // the rest token by token, the loads of four (token, element pair) items in flight per thread
-    const int n_items = n_rest_s * (D / 2);
+    const int n_items = win.n_rest * (D / 2);
     for (int i0 = tid; i0 < n_items; i0 += 4 * 128) {
         __nv_bfloat162 kk[4], vv[4];
 #pragma unroll
@@ -274,6 +292,267 @@ int32_t launch_append(mkv_pool* p, const void* k, const void* v, const int32_t* 
     }
     MKV_CUDA(cudaGetLastError());
     return MKV_OK;
+}
+
+// ------------------------------------------------------------------------------- append with rotation
+// Queries and keys are turned by their positions on the way: pair j of a head, (x, y) at dims (j, j + R/2) or, interleaved,
+// (2j, 2j + 1), becomes m (x cos - y sin), m (y cos + x sin) at the angle position * inv_freq_j.  The angle is kept in
+// 64-bit fractions of a turn, position * turns_j mod 2^64: exact for every position, where fp32 loses the fraction of a
+// turn as positions grow (2e-3 rad at 32,768, 0.06 rad at a million).  Sines and cosines are of the top 32 bits, in fp32.
+// Keys go from fp32 to e4m3 without a rounding in between; values as in Append.
+//
+// Both kernels give a thread 16 dims of a head ("unit" u): 8 pairs, which are two 16-byte chunks R/2 dims apart, or 16 dims
+// in a row (interleaved, and dims from R on, which pass as they are).
+struct RotaryArgs {
+    const uint16_t *q, *k, *v;               // bf16; token strides in elements
+    uint16_t* q_out;
+    long long q_stride, k_stride, v_stride, out_stride;
+    const int32_t *slots, *positions;        // positions [axes][n]
+    const unsigned long long* turns;         // [rotary_dim / 2]
+    const uint8_t* axis;                     // [rotary_dim / 2], or null: axis 0
+    int n, units;                            // units of a head that turn: rotary_dim / 16
+    int n_axes;
+    float mscale;
+    uint8_t* fp8;
+    int fp8_pages, hkv, group, tiles;
+    float inv_k_scale, inv_v_scale;
+    uint32_t* status;
+};
+
+struct Turn {
+    float c[8], s[8];
+};
+
+__device__ __forceinline__ void turn_of(Turn& t, const RotaryArgs& A, int token, int u)
+{
+    int p = A.positions[token];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int j = 8 * u + i;
+        if (A.axis) p = A.positions[(size_t)min((int)A.axis[j], A.n_axes - 1) * A.n + token];
+        const unsigned long long f = (unsigned long long)(long long)p * A.turns[j];
+        sincospif((float)(int)(f >> 32) * 4.656612873077393e-10f, &t.s[i], &t.c[i]);    // 2^-31: half turns
+        t.c[i] *= A.mscale;
+        t.s[i] *= A.mscale;
+    }
+}
+
+__device__ __forceinline__ void load_unit(float (&x)[16], const uint16_t* lo, const uint16_t* hi)
+{
+    const uint4 a = *reinterpret_cast<const uint4*>(lo), b = *reinterpret_cast<const uint4*>(hi);
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+
+template <bool INTERLEAVED>
+__device__ __forceinline__ void turn_unit(float (&x)[16], const Turn& t)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float& a = x[INTERLEAVED ? 2 * i : i];
+        float& b = x[INTERLEAVED ? 2 * i + 1 : 8 + i];
+        const float u = a, w = b;
+        a = u * t.c[i] - w * t.s[i];
+        b = w * t.c[i] + u * t.s[i];
+    }
+}
+
+__device__ __forceinline__ uint4 to_bf16x8(const float* x)
+{
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+        o[i] = *reinterpret_cast<const uint32_t*>(&p);
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+__device__ __forceinline__ uint2 to_e4m3x8(const float* x, float inv_scale)
+{
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        o[i] = __nv_cvt_float2_to_fp8x2(make_float2(__fmul_rn(x[2 * i], inv_scale), __fmul_rn(x[2 * i + 1], inv_scale)), __NV_SATFINITE,
+                                        __NV_E4M3);
+    return make_uint2(o[0] | (o[1] << 16), o[2] | (o[3] << 16));
+}
+
+// record of a token's slot, or null (no slot; a slot beyond the store is flagged)
+template <int D>
+__device__ __forceinline__ uint8_t* record_of(const RotaryArgs& A, int slot, int h, bool flag)
+{
+    if (slot < 0) return nullptr;
+    const int gt = slot >> 4, page = gt / A.tiles;
+    if (page >= A.fp8_pages) {
+        if (flag) atomicOr(A.status, kStBounds);
+        return nullptr;
+    }
+    return A.fp8 + (((size_t)page * A.hkv + h) * A.tiles + (gt - page * A.tiles)) * fp8_record_bytes(D);
+}
+
+// dims of a unit: the first of its two chunks, and how far the second lies
+template <bool INTERLEAVED>
+__device__ __forceinline__ void unit_dims(const RotaryArgs& A, int u, int& lo, int& hi)
+{
+    const bool apart = !INTERLEAVED && u < A.units;
+    lo = apart ? 8 * u : 16 * u;
+    hi = apart ? 8 * A.units + 8 * u : lo + 8;
+}
+
+// Decode-sized calls: a block per (token, KV head), a thread per unit of one of its query heads, its key or its value.
+// Bound by latency: position, slot, inputs and frequencies are loaded at once, sines and stores follow.
+template <int D, bool INTERLEAVED>
+__global__ void __launch_bounds__((kMaxGroup + 2) * D / 16) append_rotary_kernel(const RotaryArgs A)
+{
+    pdl_begin();
+    const int tok = blockIdx.x, h = blockIdx.y, u = threadIdx.x % (D / 16), item = threadIdx.x / (D / 16);
+    const int n_q = A.q ? A.group : 0;                       // items: query heads, then key, then value
+    const bool is_q = item < n_q, is_v = item == n_q + 1;
+    float x[16];
+    int lo, hi;
+    unit_dims<INTERLEAVED>(A, u, lo, hi);
+    if (is_v) { lo = 16 * u; hi = lo + 8; }
+    const uint16_t* src = is_q ? A.q + (size_t)tok * A.q_stride + (size_t)(h * A.group + item) * D
+                               : (is_v ? A.v + (size_t)tok * A.v_stride : A.k + (size_t)tok * A.k_stride) + (size_t)h * D;
+    load_unit(x, src + lo, src + hi);
+    const int slot = is_q ? -1 : A.slots[tok];
+    if (!is_v && u < A.units) {
+        Turn t;
+        turn_of(t, A, tok, u);
+        turn_unit<INTERLEAVED>(x, t);
+    }
+    if (is_q) {
+        uint16_t* dst = A.q_out + (size_t)tok * A.out_stride + (size_t)(h * A.group + item) * D;
+        *reinterpret_cast<uint4*>(dst + lo) = to_bf16x8(x);
+        *reinterpret_cast<uint4*>(dst + hi) = to_bf16x8(x + 8);
+        return;
+    }
+    uint8_t* rec = record_of<D>(A, slot, h, u == 0 && !is_v);
+    if (!rec) return;
+    const uint2 a = to_e4m3x8(x, is_v ? A.inv_v_scale : A.inv_k_scale), b = to_e4m3x8(x + 8, is_v ? A.inv_v_scale : A.inv_k_scale);
+    if (!is_v) {
+        uint8_t* row = rec + (slot & 15) * D;
+        *reinterpret_cast<uint2*>(row + lo) = a;
+        *reinterpret_cast<uint2*>(row + hi) = b;
+        return;
+    }
+    const uint32_t w[4] = {a.x, a.y, b.x, b.y};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) rec[16 * D + (lo + i) * kPage + (slot & 15)] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+}
+
+// Prefill-sized calls: a block per (window of 16 tokens, KV head), a thread per (token, unit): its sines serve the key and
+// the whole query group.  Keys are written token by token (rows of a record).  Values take the runs that start in the
+// window, as in append_run_kernel: whole tiles leave through shared memory as 16-byte channels.
+template <int D, bool INTERLEAVED>
+__global__ void __launch_bounds__(D) append_rotary_run_kernel(const RotaryArgs A)
+{
+    constexpr int VROW = D + 4, UNITS = D / 16;
+    __shared__ __align__(16) uint8_t vt[kPage * VROW];
+    __shared__ RunWindow win;
+    pdl_begin();
+    const int t0 = blockIdx.x * kPage, h = blockIdx.y, tid = threadIdx.x, t = tid / UNITS, u = tid % UNITS, tok = t0 + t;
+    const bool live = tok < A.n;
+    if (tid < 32 && A.k) find_runs(win, A.slots, A.n, t0, A.tiles, A.fp8_pages, tid);
+    Turn turn;
+    if (live && u < A.units) turn_of(turn, A, tok, u);
+    int lo, hi;
+    unit_dims<INTERLEAVED>(A, u, lo, hi);
+    __syncthreads();
+    const int full = A.k ? win.full : -1;
+    float val[16];
+    if (full >= 0) {
+        const uint16_t* src = A.v + (size_t)(t0 + full + t) * A.v_stride + (size_t)h * D + 16 * u;
+        load_unit(val, src, src + 8);
+    }
+    if (live && A.k) {
+        const int slot = win.slot[t];
+        uint8_t* rec = record_of<D>(A, slot, h, u == 0);
+        if (rec) {
+            float x[16];
+            const uint16_t* src = A.k + (size_t)tok * A.k_stride + (size_t)h * D;
+            load_unit(x, src + lo, src + hi);
+            if (u < A.units) turn_unit<INTERLEAVED>(x, turn);
+            uint8_t* row = rec + (slot & 15) * D;
+            *reinterpret_cast<uint2*>(row + lo) = to_e4m3x8(x, A.inv_k_scale);
+            *reinterpret_cast<uint2*>(row + hi) = to_e4m3x8(x + 8, A.inv_k_scale);
+        }
+    }
+    if (live && A.q) {
+        const uint16_t* src = A.q + (size_t)tok * A.q_stride + (size_t)h * A.group * D;
+        uint16_t* dst = A.q_out + (size_t)tok * A.out_stride + (size_t)h * A.group * D;
+#pragma unroll 2
+        for (int i = 0; i < A.group; ++i, src += D, dst += D) {
+            float x[16];
+            load_unit(x, src + lo, src + hi);
+            if (u < A.units) turn_unit<INTERLEAVED>(x, turn);
+            *reinterpret_cast<uint4*>(dst + lo) = to_bf16x8(x);
+            *reinterpret_cast<uint4*>(dst + hi) = to_bf16x8(x + 8);
+        }
+    }
+    if (full >= 0) {
+        const uint2 a = to_e4m3x8(val, A.inv_v_scale), b = to_e4m3x8(val + 8, A.inv_v_scale);
+        uint32_t* row = reinterpret_cast<uint32_t*>(vt + t * VROW + 16 * u);
+        row[0] = a.x; row[1] = a.y; row[2] = b.x; row[3] = b.y;
+        __syncthreads();
+        store_value_tile<D, D>(record_of<D>(A, win.slot[full], h, false), vt, tid);
+    }
+    // values of the other runs, token by token
+    const int n_items = A.k ? win.n_rest * UNITS : 0;
+    for (int i = tid; i < n_items; i += D) {
+        const int at = win.rest[i / UNITS], slot = win.slot[at], c = i % UNITS;
+        uint8_t* rec = record_of<D>(A, slot, h, false);              // flagged with its key
+        if (!rec) continue;
+        float x[16];
+        const uint16_t* src = A.v + (size_t)(t0 + at) * A.v_stride + (size_t)h * D + 16 * c;
+        load_unit(x, src, src + 8);
+        const uint2 a = to_e4m3x8(x, A.inv_v_scale), b = to_e4m3x8(x + 8, A.inv_v_scale);
+        const uint32_t w[4] = {a.x, a.y, b.x, b.y};
+#pragma unroll
+        for (int e = 0; e < 16; ++e) rec[16 * D + (16 * c + e) * kPage + (slot & 15)] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
+    }
+}
+
+template <int D, bool INTERLEAVED>
+static int32_t launch_rotary(const RotaryArgs& A, cudaStream_t s)
+{
+    if (A.n >= kAppendRun)
+        MKV_CUDA(launch_pdl(append_rotary_run_kernel<D, INTERLEAVED>, dim3((A.n + kPage - 1) / kPage, A.hkv), D, 0, 1, s, A));
+    else
+        MKV_CUDA(launch_pdl(append_rotary_kernel<D, INTERLEAVED>, dim3(A.n, A.hkv), ((A.q ? A.group : 0) + (A.k ? 2 : 0)) * D / 16, 0, 1,
+                            s, A));
+    MKV_CUDA(cudaGetLastError());
+    return MKV_OK;
+}
+
+int32_t launch_append_rotary(mkv_pool* p, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                             int64_t v_stride, const int32_t* slots, const int32_t* positions, int n, const mkv_rotary* r, void* q_out,
+                             int64_t out_stride, cudaStream_t s)
+{
+    RotaryArgs A = {};
+    A.q = static_cast<const uint16_t*>(q);
+    A.k = static_cast<const uint16_t*>(k);
+    A.v = static_cast<const uint16_t*>(v);
+    A.q_out = static_cast<uint16_t*>(q_out);
+    A.q_stride = q_stride; A.k_stride = k_stride; A.v_stride = v_stride; A.out_stride = out_stride;
+    A.slots = slots; A.positions = positions;
+    A.turns = reinterpret_cast<const unsigned long long*>(r->turns_dev);
+    A.axis = r->axis_dev;
+    A.n = n;
+    A.units = r->rotary_dim / 16;
+    A.n_axes = r->n_axes;
+    A.mscale = r->mscale;
+    A.fp8 = p->fp8;
+    A.fp8_pages = p->cfg.fp8_pages; A.hkv = p->hkv; A.group = p->group; A.tiles = p->tiles;
+    A.inv_k_scale = 1.0f / p->cfg.k_scale; A.inv_v_scale = 1.0f / p->cfg.v_scale;
+    A.status = p->status_dev;
+    if (p->d == 128) return r->interleaved ? launch_rotary<128, true>(A, s) : launch_rotary<128, false>(A, s);
+    return r->interleaved ? launch_rotary<256, true>(A, s) : launch_rotary<256, false>(A, s);
 }
 
 // ---- thread-block cluster helpers (Demote and Promote run one cluster per page) ------------------

@@ -182,6 +182,9 @@ int32_t launch_append_layers(mkv_pool* const* pools, const void* const* k, const
                              int n_tokens, int n_layers, cudaStream_t s);
 int32_t launch_page_score(const float* mass, const int32_t* lens, int B, int hq, int max_pages, uint64_t head_mask,
                           float beta, float* score, int page_tokens, cudaStream_t s);
+int32_t launch_append_rotary(mkv_pool* p, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                             int64_t v_stride, const int32_t* slots, const int32_t* positions, int n, const mkv_rotary* r, void* q_out,
+                             int64_t out_stride, cudaStream_t s);
 int32_t launch_chunk_attention(mkv_pool* p, const void* q, int64_t q_stride, int n_rows, const int32_t* starts, const int32_t* bt,
                                const uint8_t* tags, const int32_t* lens, int B, int max_pages, float scale, void* out, float* lse,
                                void* ws, cudaStream_t s);

@@ -2,6 +2,7 @@
 // argument validation and the C ABI entry points.  No arithmetic of the method lives here.
 #include <cstdio>
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <new>
 #include <string>
@@ -286,6 +287,42 @@ int32_t mkv_append(mkv_pool* pool, const void* k, const void* v, const int32_t* 
     if (n == 0) return MKV_OK;
     if (!k || !v || !slots || !aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 4)) return MKV_E_INVALID;
     return launch_append(pool, k, v, slots, n, (cudaStream_t)stream);
+}
+
+int32_t mkv_rotary_turns(const double* inv_freq, int32_t n, uint64_t* turns)
+{
+    if (n < 0 || (n > 0 && (!inv_freq || !turns))) return MKV_E_INVALID;
+    for (int i = 0; i < n; ++i) {
+        if (!(inv_freq[i] - inv_freq[i] == 0.0)) return MKV_E_INVALID;        // infinite, or not a number
+        // whole turns leave every (integer) position where it is: only the fraction is kept
+        const long double pi = 3.141592653589793238462643383279502884L;
+        long double t = static_cast<long double>(inv_freq[i]) / (2 * pi);
+        t -= floorl(t);
+        const long double scaled = roundl(t * 18446744073709551616.0L);
+        turns[i] = scaled >= 18446744073709551616.0L ? 0 : static_cast<uint64_t>(scaled);
+    }
+    return MKV_OK;
+}
+
+int32_t mkv_append_rotary(mkv_pool* pool, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                          int64_t v_stride, const int32_t* slots, const int32_t* positions, int32_t n, const mkv_rotary* r,
+                          void* q_out, int64_t out_stride, void* stream)
+{
+    if (!pool || !pool->fp8 || n < 0 || !r) return MKV_E_INVALID;
+    if (r->rotary_dim < 16 || r->rotary_dim > pool->d || r->rotary_dim % 16 || r->n_axes < 1 || r->n_axes > 256 || !r->turns_dev ||
+        !aligned(r->turns_dev, 8) || (r->n_axes > 1 && !r->axis_dev) || !(r->mscale - r->mscale == 0.f))
+        return MKV_E_INVALID;
+    if (n == 0) return MKV_OK;
+    if ((!q && !k) || !q != !q_out || !k != !v || (k && !slots) || !positions) return MKV_E_INVALID;
+    const int64_t row_q = (int64_t)pool->hq * pool->d, row_kv = (int64_t)pool->hkv * pool->d;
+    if (q && (q_stride < row_q || q_stride % 8 || out_stride < row_q || out_stride % 8 || !aligned(q, 16) || !aligned(q_out, 16)))
+        return MKV_E_INVALID;
+    if (k && (k_stride < row_kv || k_stride % 8 || v_stride < row_kv || v_stride % 8 || !aligned(k, 16) || !aligned(v, 16) ||
+              !aligned(slots, 4)))
+        return MKV_E_INVALID;
+    if (!aligned(positions, 4)) return MKV_E_INVALID;
+    return launch_append_rotary(pool, q, q_stride, k, k_stride, v, v_stride, slots, positions, n, r, q_out, out_stride,
+                                (cudaStream_t)stream);
 }
 
 int32_t mkv_demote(mkv_pool* pool, const int32_t* src, const int32_t* dst, int32_t n, int32_t* bt,

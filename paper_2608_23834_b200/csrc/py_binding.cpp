@@ -213,6 +213,41 @@ bool is_rows(const at::Tensor* t, int64_t n, int64_t heads, int64_t d, int64_t* 
     return *stride >= heads * d && *stride % 8 == 0;
 }
 
+// append_rotary(ref, q, k, v, slot_mapping, positions, address of the mkv_rotary, its turns, its axes, q_out, stream)
+PyObject* append_rotary(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    const PoolRef* r = n == 11 ? ref_of(a[0]) : nullptr;
+    if (!r) return result(kCheck);
+    const at::Tensor *q = tensor(a[1]), *k = tensor(a[2]), *v = tensor(a[3]), *slots = tensor(a[4]), *pos = tensor(a[5]),
+                     *turns = tensor(a[7]), *out = tensor(a[9]);
+    const auto* rot = static_cast<const mkv_rotary*>(PyLong_AsVoidPtr(a[6]));
+    const long axes = PyLong_AsLong(a[8]);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        return result(kCheck);
+    }
+    // the whole call only (queries, keys and values); the others go through the Python checks
+    if (!q || q->dim() != 3 || !turns || !rot) return result(kCheck);
+    const int64_t tokens = q->size(0);
+    int64_t sq, sk, sv, so;
+    if (!is_rows(q, tokens, r->hq, r->d, &sq) || !is_rows(out, tokens, r->hq, r->d, &so) || !is_rows(k, tokens, r->hkv, r->d, &sk) ||
+        !is_rows(v, tokens, r->hkv, r->d, &sv) || !is_dense(slots, at::kInt) || slots->numel() != tokens || !is_dense(pos, at::kInt))
+        return result(kCheck);
+    if (!(pos->dim() == 2 && pos->size(0) == axes && pos->size(1) == tokens) && !(axes == 1 && pos->dim() == 1 && pos->size(0) == tokens))
+        return result(kCheck);
+    const c10::Device dev(c10::kCUDA, (c10::DeviceIndex)r->device);
+    if (q->device() != dev || k->device() != dev || v->device() != dev || slots->device() != dev || pos->device() != dev ||
+        turns->device() != dev || out->device() != dev)
+        return result(kCheck);
+    const c10::cuda::CUDAGuard guard(dev);
+    void* s;
+    if (!stream_of(a[10], &s)) return result(kCheck);
+    const void *qp = q->data_ptr(), *kp = k->data_ptr(), *vp = v->data_ptr();
+    const auto *sp = static_cast<const int32_t*>(slots->data_ptr()), *pp = static_cast<const int32_t*>(pos->data_ptr());
+    void* op = out->data_ptr();
+    return enqueue([=] { return mkv_append_rotary(r->pool, qp, sq, kp, sk, vp, sv, sp, pp, (int)tokens, rot, op, so, s); });
+}
+
 // None or a dense fp32 tensor of [n][heads]
 bool optional_lse(PyObject* o, int64_t n, int64_t heads, void** ptr)
 {
@@ -398,7 +433,7 @@ PyMethodDef methods[] = {
     FAST("pool_ref", pool_ref), FAST("append", append), FAST("demote", convert<mkv_demote>), FAST("promote", convert<mkv_promote>),
     FAST("decode", decode), FAST("decode_scored", decode_scored), FAST("decode_layers", decode_layers),
     FAST("append_layers", append_layers), FAST("score_update", score_update),
-    FAST("chunk_attention", chunk_attention), {nullptr, nullptr, 0, nullptr}};
+    FAST("append_rotary", append_rotary), FAST("chunk_attention", chunk_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mkv_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
