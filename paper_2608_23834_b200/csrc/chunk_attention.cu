@@ -86,13 +86,17 @@ struct Geo {
     static constexpr int STAGES = D == 128 ? 2 : 1;             // key tiles, and value tiles, in shared memory
     static constexpr int Q_TILE = 128 * D * 2, K_TILE = kKeys * D * 2, V_TILE = K_TILE;
     static constexpr int SOFT_WARPS = 4 * NT, UNPACK_WARPS = 8;
-    static constexpr int MMA_WARP = SOFT_WARPS + UNPACK_WARPS, THREADS = 32 * (MMA_WARP + 1);
+    static constexpr int MMA_WARP = SOFT_WARPS + UNPACK_WARPS, THREADS = 32 * (MMA_WARP + 4);
+    // registers: of the launch, and of the softmax, unpacking and product warps afterwards (the sums agree)
+    static constexpr int REGS = D == 128 ? 96 : 128;
+    static constexpr int SOFT_REGS = D == 128 ? 104 : 144, UNPACK_REGS = D == 128 ? 104 : 144, MMA_REGS = D == 128 ? 64 : 80;
+    static_assert(SOFT_WARPS * SOFT_REGS + UNPACK_WARPS * UNPACK_REGS + 4 * MMA_REGS <= (MMA_WARP + 4) * REGS, "register split");
     static constexpr int OFF_Q = 0, OFF_K = OFF_Q + NT * Q_TILE, OFF_V = OFF_K + STAGES * K_TILE;
     static constexpr int OFF_FAC = OFF_V + STAGES * V_TILE;     // factor of every row's scores
     static constexpr int OFF_NAN = OFF_FAC + ROWS * 4;          // 64-bit word per channel, see note_nan
     static constexpr int OFF_BAR = OFF_NAN + D * 8;
     static constexpr int OFF_MISC = OFF_BAR + 256;
-    static constexpr int SMEM = OFF_MISC + 64 + 1024;           // the tiles start on a 1,024-byte boundary
+    static constexpr int SMEM = OFF_MISC + 128 + 1024;           // the tiles start on a 1,024-byte boundary
     static_assert(SMEM <= 232448, "shared memory of a block");
 };
 
@@ -101,7 +105,9 @@ enum {
     kKFull = 0, kKEmpty = 2, kVFull = 4, kVEmpty = 6,           // [stage]
     kSFull = 8, kPFull = 10,                                    // [score buffer]
     kPvDone = 12,                                               // [row tile]
-    kQFull = 14, kFacRead = 15, kSegDone = 16, kDrained = 17, kBars = 18
+    kQFull = 14, kFacRead = 15, kSegDone = 16, kDrained = 17,
+    kOutput = 18,                                               // [row tile] the last product of a segment
+    kBars = 20
 };
 
 // ---- the units --------------------------------------------------------------------------------------
@@ -133,42 +139,45 @@ struct Segment {
     int last_block;
 };
 
-// Walks the units that the positions [p0, p1) of the cut meet; every thread of a block does so by itself.
+// A block's share [p0, p1) of the units laid end to end (shared memory), and where its first unit's request begins.
+struct Share {
+    long long p0, p1, per, request_start;
+    int request;
+};
+
+// Walks the units that a block's share meets; every thread of a block does so by itself.
 template <int ROWS>
 struct Walker {
-    const Params& P;
-    long long p0, p1, at, per;
-    int b, h, rt, block;
-    Request r;
+    long long at;
+    int b, h, rt;
 
-    __device__ __forceinline__ Walker(const Params& P_, long long p0_, long long p1_, long long per_, int b_, long long request_start)
-        : P(P_), p0(p0_), p1(p1_), at(request_start), per(per_), b(b_), h(0), rt(0), block(blockIdx.x)
+    __device__ __forceinline__ Walker(const Params& P, const Share* share) : at(share->request_start), b(share->request), h(0), rt(0)
     {
-        r = P.req[b];
-        const long long skip = (p0 - at) / r.cost;              // KV heads before the first unit
+        const long long cost = P.req[b].cost, skip = (share->p0 - at) / cost;       // KV heads before the first unit
         h = (int)skip;
-        at += skip * r.cost;
+        at += skip * cost;
     }
-    __device__ __forceinline__ bool next(Segment& s)
+    __device__ __forceinline__ bool next(const Params& P, const Share* share, Segment& s)
     {
+        const long long p0 = share->p0, p1 = share->p1;
         while (at < p1 && b < P.B) {
-            const int n_rt = (r.n_new * P.group + ROWS - 1) / ROWS;
+            s.r = P.req[b];
+            const int n_rt = (s.r.n_new * P.group + ROWS - 1) / ROWS;
             if (n_rt == 0) {
-                if (++b < P.B) r = P.req[b];
+                ++b;
                 continue;
             }
-            s.r = r;
-            s.u = unit_of<ROWS>(r, P.group, rt);
+            s.u = unit_of<ROWS>(s.r, P.group, rt);
             const int n = s.u.stale_tiles + s.u.fp8_tiles;
             const long long start = at, first = at + kUnitCost;
             s.b = b; s.h = h; s.rt = rt;
-            s.nt = min(ROWS / 128, (r.n_new * P.group - rt * ROWS + 127) / 128);
+            s.nt = min(ROWS / 128, (s.r.n_new * P.group - rt * ROWS + 127) / 128);
             at = first + n;
             if (++rt == n_rt) {
                 rt = 0;
                 if (++h == P.hkv) {
                     h = 0;
-                    if (++b < P.B) r = P.req[b];
+                    ++b;
                 }
             }
             s.t0 = (int)max(0ll, p0 - first);
@@ -176,9 +185,9 @@ struct Walker {
             if (n == 0) s.t0 = s.t1 = 0;                         // rows that see nothing
             if (s.t1 > s.t0 || (n == 0 && start >= p0)) {
                 const bool whole = s.t0 == 0 && s.t1 == n;
-                s.slot = whole ? -1 : 2 * block + (start >= p0 ? 1 : 0);
+                s.slot = whole ? -1 : 2 * (int)blockIdx.x + (start >= p0 ? 1 : 0);
                 s.first_part = !whole && s.t0 == 0;
-                s.last_block = (int)((first + n - 1) / per);
+                s.last_block = (int)((first + n - 1) / share->per);
                 return true;
             }
         }
@@ -322,6 +331,16 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&r)[32])
                    "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
                  : "r"(taddr) : "memory");
 }
+// waits for the loads so far; the values pass through, so that nothing computed from them is moved before the wait
+__device__ __forceinline__ void tmem_wait_ld32(float (&r)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]), "+f"(r[8]),
+                   "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]), "+f"(r[16]),
+                   "+f"(r[17]), "+f"(r[18]), "+f"(r[19]), "+f"(r[20]), "+f"(r[21]), "+f"(r[22]), "+f"(r[23]), "+f"(r[24]),
+                   "+f"(r[25]), "+f"(r[26]), "+f"(r[27]), "+f"(r[28]) :: "memory");
+    asm volatile("" : "+f"(r[29]), "+f"(r[30]), "+f"(r[31]) :: "memory");
+}
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&r)[32])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
@@ -343,12 +362,8 @@ __device__ __forceinline__ uint32_t hmul2_u32(uint32_t a, uint32_t b)
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
-// true where one of the two fp16 is NaN
-__device__ __forceinline__ bool has_nan2(uint32_t x)
-{
-    const __half2 h = *reinterpret_cast<const __half2*>(&x);
-    return __hisnan(__low2half(h)) || __hisnan(__high2half(h));
-}
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2*>(&x); }
+__device__ __forceinline__ uint32_t as_u32(__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); }
 __device__ __forceinline__ uint4 ldg128(const void* p)          // coherent: pages may have been written by the kernel before
 {
     uint4 v;
@@ -359,6 +374,12 @@ __device__ __forceinline__ uint2 ldg64(const void* p)
 {
     uint2 v;
     asm volatile("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint32_t ldg16(const void* p)
+{
+    uint16_t v;
+    asm volatile("ld.global.u16 %0, [%1];" : "=h"(v) : "l"(p));
     return v;
 }
 __device__ __forceinline__ uint32_t ldg32(const void* p)
@@ -383,9 +404,46 @@ __device__ __forceinline__ int stale_row(int e, int t)
 {
     return 64 * (e >> 2) + 8 * (2 * ((t & 7) >> 1) + ((e >> 1) & 1)) + 4 * (e & 1) + 2 * (t >> 3) + (t & 1);
 }
-// ... and back: run and token of key row n
-__device__ __forceinline__ int run_of_row(int n) { return 4 * (n >> 6) + 2 * ((n >> 3) & 1) + ((n >> 2) & 1); }
-__device__ __forceinline__ int token_of_row(int n) { return 2 * ((n >> 4) & 3) + (n & 1) + 8 * ((n >> 1) & 1); }
+// So key row n is token 2 (n / 16 mod 4) + 8 (n / 2 mod 2) + n mod 2 of run 4 (n / 64) + 2 (n / 8 mod 2) + n / 4 mod 2.
+
+// Entry of a run of 16 tokens in a list, looked up one key tile (eight runs) ahead of its use.
+struct Cursor {
+    const int2* list;
+    int page, sub, run, n, tiles, step;       // step: 1, or -1 for the list that grows from the back
+    int2 entry;                               // logical page, id; valid where ok
+    bool ok;
+
+    __device__ __forceinline__ void open(const int2* l, int r, int count, int t, int direction)
+    {
+        list = l; run = r; n = count; tiles = t; step = direction;
+        page = r / t;
+        sub = r - page * t;
+        look();
+    }
+    __device__ __forceinline__ void look()
+    {
+        ok = run < n;
+        entry = make_int2(0, 0);
+        if (ok) {
+            const uint2 v = ldg64(list + (long long)step * page);
+            entry = make_int2((int)v.x, (int)v.y);
+        }
+    }
+    __device__ __forceinline__ void next()
+    {
+        run += 8;
+        if (tiles == 1) page += 8;
+        else {
+            sub += 8;
+            if (sub >= tiles) {
+                const int q = sub / tiles;
+                page += q;
+                sub -= q * tiles;
+            }
+        }
+        look();
+    }
+};
 
 // ---- scan -------------------------------------------------------------------------------------------
 template <int D, int FMT>
@@ -402,8 +460,8 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
     unsigned long long* nan_s = reinterpret_cast<unsigned long long*>(smem + G::OFF_NAN);
     volatile int* failed_s = reinterpret_cast<volatile int*>(smem + G::OFF_MISC);
     uint32_t* tmem_s = reinterpret_cast<uint32_t*>(smem + G::OFF_MISC + 4);
-    int* start_b_s = reinterpret_cast<int*>(smem + G::OFF_MISC + 8);
-    long long* start_s = reinterpret_cast<long long*>(smem + G::OFF_MISC + 16);   // request's first position, total
+    volatile uint32_t* noted_s = reinterpret_cast<volatile uint32_t*>(smem + G::OFF_MISC + 8);    // segment of the latest note
+    Share* share = reinterpret_cast<Share*>(smem + G::OFF_MISC + 16);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     auto bar = [&](int i) -> uint32_t { return sb + G::OFF_BAR + 8 * i; };
 
@@ -416,6 +474,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
             mbar_init(bar(i), count);
         }
         *failed_s = 0;
+        *noted_s = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     for (int i = tid; i < D; i += G::THREADS) nan_s[i] = 0;
@@ -448,25 +507,23 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
             before += __shfl_sync(FULL, s, 31);
         }
         if (lane == 0) {
-            *start_b_s = found;
-            start_s[0] = at;
-            start_s[1] = total;
-            start_s[2] = per;
+            share->request = found;
+            share->request_start = at;
+            share->p0 = p0;
+            share->p1 = min(total, p0 + per);
+            share->per = per;
         }
     }
     __syncthreads();
-    const int b0 = *start_b_s;
-    const long long total = start_s[1], per = start_s[2];
     if (tid == 0) P.merge[blockIdx.x].b = -1;
-    if (b0 < 0) return;                                          // nothing to do (and nothing allocated yet)
+    if (share->request < 0) return;                                          // nothing to do (and nothing allocated yet)
     if (warp == G::MMA_WARP) tmem_alloc(smem_u32(tmem_s), 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tb = *tmem_s;
     constexpr uint32_t kColS = NT * D;                           // O: NT x D columns, then two score buffers
-    const long long p0 = per * blockIdx.x, p1 = min(total, p0 + per);
-    Walker<ROWS> walk(P, p0, p1, per, b0, start_s[0]);
+    Walker<ROWS> walk(P, share);
     Segment s;
 
     // bounded by wall time: a wait that gives up flags the pool and lets every later wait of the block pass
@@ -487,45 +544,52 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
         }
     };
 
-    if (warp == G::MMA_WARP) {
+    if (warp >= G::MMA_WARP) {
         // ================= products =================
-        if (lane == 0) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(G::MMA_REGS));
+        if (warp == G::MMA_WARP && lane == 0) {
             uint32_t job = 0, tile = 0, fills = 0;               // scores, key tiles and queries so far
-            while (walk.next(s)) {
+            while (walk.next(P, share, s)) {
                 const int n = (s.t1 - s.t0) * s.nt, cut = s.u.stale_tiles;
-                auto scores = [&](int i) {                       // job i of the segment: key tile t0 + i / nt, row tile i % nt
-                    const int j = i / s.nt, t = i - j * s.nt, kt = s.t0 + j;
-                    const uint32_t at = tile + j, st = at % G::STAGES, buf = (job + i) & 1;
-                    if (t == 0) {
-                        if (j == 0 || kt == cut) wait(kQFull, fills++ & 1);
-                        wait(kKFull + st, (at / G::STAGES) & 1);
+                // job i of the segment: key tile t0 + i / nt, row tile i % nt; its scores are issued two jobs ahead
+                for (int i = -2; i < n; ++i) {
+                    if (i >= 0) {
+                        const int j = s.nt == 2 ? i >> 1 : i, t = s.nt == 2 ? i & 1 : 0;
+                        const uint32_t at = tile + j, st = at % G::STAGES, buf = (job + i) & 1;
+                        if (t == 0) wait(kVFull + st, (at / G::STAGES) & 1);
+                        wait(kPFull + buf, ((job + i) >> 1) & 1);
                         tc_fence_after();
-                    }
-                    const uint64_t a = operand_desc(sb + G::OFF_Q + t * G::Q_TILE), k = operand_desc(sb + G::OFF_K + st * G::K_TILE);
+                        const uint64_t v = operand_desc(sb + G::OFF_V + st * G::V_TILE);
+                        const uint32_t o = tb + t * D, p = tb + kColS + kKeys * buf;
+#pragma unroll 1
+                        for (int half = 0; half < 2; ++half)
 #pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk) {
-                        const uint64_t step = ((kk >> 2) * (128 * 128) + (kk & 3) * 32) >> 4;
-                        mma_ss(tb + kColS + kKeys * buf, a + step, k + step, idesc(kKeys), kk > 0);
+                            for (int kk = 0; kk < 4; ++kk)
+                                mma_ts(o, p + 32 * half + 8 * kk, v + ((half * (D * 128) + kk * 32) >> 4), idesc(D), j > 0 || half > 0 || kk > 0);
+                        mma_commit(bar(kPvDone + t));
+                        if (i + s.nt >= n) mma_commit(bar(kOutput + t));
+                        if (t == s.nt - 1) mma_commit(bar(kVEmpty + st));
                     }
-                    mma_commit(bar(kSFull + buf));
-                    if (t == s.nt - 1) mma_commit(bar(kKEmpty + st));
-                };
-                if (n > 0) scores(0);
-                if (n > 1) scores(1);
-                for (int i = 0; i < n; ++i) {
-                    const int j = i / s.nt, t = i - j * s.nt;
-                    const uint32_t at = tile + j, st = at % G::STAGES, buf = (job + i) & 1;
-                    if (t == 0) wait(kVFull + st, (at / G::STAGES) & 1);
-                    wait(kPFull + buf, ((job + i) >> 1) & 1);
-                    tc_fence_after();
-                    const uint64_t v = operand_desc(sb + G::OFF_V + st * G::V_TILE);
+                    if (i + 2 < n) {
+                        const int i2 = i + 2, j = s.nt == 2 ? i2 >> 1 : i2, t = s.nt == 2 ? i2 & 1 : 0;
+                        const uint32_t at = tile + j, st = at % G::STAGES, buf = (job + i2) & 1;
+                        if (t == 0) {
+                            if (j == 0 || s.t0 + j == cut) wait(kQFull, fills++ & 1);
+                            wait(kKFull + st, (at / G::STAGES) & 1);
+                            tc_fence_after();
+                        }
+                        const uint64_t a = operand_desc(sb + G::OFF_Q + t * G::Q_TILE), k = operand_desc(sb + G::OFF_K + st * G::K_TILE);
+                        const uint32_t d = tb + kColS + kKeys * buf;
+#pragma unroll 1
+                        for (int atom = 0; atom < D / 64; ++atom)
 #pragma unroll
-                    for (int kk = 0; kk < kKeys / 16; ++kk)
-                        mma_ts(tb + t * D, tb + kColS + kKeys * buf + 8 * kk, v + (((kk >> 2) * (D * 128) + (kk & 3) * 32) >> 4), idesc(D),
-                               j > 0 || kk > 0);
-                    mma_commit(bar(kPvDone + t));
-                    if (t == s.nt - 1) mma_commit(bar(kVEmpty + st));
-                    if (i + 2 < n) scores(i + 2);
+                            for (int kk = 0; kk < 4; ++kk) {
+                                const uint64_t step = (atom * (128 * 128) + kk * 32) >> 4;
+                                mma_ss(d, a + step, k + step, idesc(kKeys), atom > 0 || kk > 0);
+                            }
+                        mma_commit(bar(kSFull + buf));
+                        if (t == s.nt - 1) mma_commit(bar(kKEmpty + st));
+                    }
                 }
                 job += n;
                 tile += s.t1 - s.t0;
@@ -545,16 +609,17 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
         __syncwarp();
     } else if (warp >= G::SOFT_WARPS) {
         // ================= queries and unpacking =================
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(G::UNPACK_REGS));
         const int w = warp - G::SOFT_WARPS, g = lane >> 2, tq = lane & 3;
         const uint32_t ku = (uint32_t)(15 - P.ke) << 10, vu = (uint32_t)(15 - P.ve) << 10;     // 2^-ke, 2^-ve as fp16
         const uint32_t k_unit = ku | ku << 16, v_unit = vu | vu << 16;
-        uint32_t tile = 0, fills = 0, segments = 0;
+        uint32_t k_tile = 0, v_tile = 0, fills = 0, segments = 0;   // key tiles and value tiles unpacked so far
         auto arrive = [&](int i) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(i));
         };
-        while (walk.next(s)) {
+        while (walk.next(P, share, s)) {
             ++segments;
             const int first_pos = s.r.len - s.r.n_new + s.rt * ROWS / P.group;        // of the unit's first row
             const int rows = min(ROWS, s.r.n_new * P.group - s.rt * ROWS);
@@ -565,7 +630,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
 
             // ---- queries of one format: a warp per row, a lane D / 32 dims
             auto fill_query = [&](bool stale) {
-                if (tile > 0) wait(kKEmpty + (tile - 1) % G::STAGES, ((tile - 1) / G::STAGES) & 1);   // the products so far are done
+                if (k_tile > 0) wait(kKEmpty + (k_tile - 1) % G::STAGES, ((k_tile - 1) / G::STAGES) & 1);   // the products so far are done
                 if (fills > 0) wait(kFacRead, (fills - 1) & 1);
                 ++fills;
                 constexpr int N = D / 32;
@@ -666,46 +731,44 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                 arrive(kQFull);
             };
 
-            // A value that is NaN is as a rule seen by every row of the tile (0 x NaN).  In a tile with masked places it
-            // is taken out and its channel's first such position noted; the epilogue gives NaN to the rows from there
-            // on.  The note carries the segment, and an older segment's epilogue is waited for before it is replaced.
-            auto note_nan = [&](int channel, int pos) {
+            // An FP8 value that is NaN is as a rule seen by every row of the tile (0 x NaN).  In a tile with masked places
+            // its bytes are cleared and the channel's first such position is noted; the epilogue gives NaN to the rows
+            // from there on.  The note carries the segment, and the epilogue of the segment before is waited for.
+            auto note_nan = [&](uint4 (&x)[16 * D / 512], int pos) {
                 if (segments > 1) wait(kSegDone, (segments - 2) & 1);
-                atomicMax(&nan_s[channel], (unsigned long long)segments << 32 | (uint32_t)(kNoPos - pos));
+#pragma unroll
+                for (int i = 0; i < 16 * D / 512; ++i) {
+                    uint32_t* word = reinterpret_cast<uint32_t*>(&x[i]);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t bad = __vcmpeq4(word[q] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+                        if (!bad) continue;
+                        const int at = pos + 4 * q + ((__ffs(bad) - 1) >> 3);
+                        atomicMax(&nan_s[i * 32 + lane], (unsigned long long)segments << 32 | (uint32_t)(kNoPos - at));
+                        *noted_s = segments;
+                        word[q] &= ~bad;
+                    }
+                }
             };
 
             const int cut = s.u.stale_tiles;
             if (s.t0 < cut) {
                 // ---- Stale tiles: keys of run w; values of the two runs w & ~1, w | 1, half of the channels
                 constexpr int LW = 3 * D / 64;                   // packed words of a lane per section
-                const int n_tiles = min(s.t1, cut);
-                const int half = w & 1;
-                const uint8_t *rec[2], *meta[2];                 // the pair's records (null: no run) and page scales
-                int pos[2];
-                auto locate = [&](int t) {
+                const int n_tiles = min(s.t1, cut), half = w & 1;
+                Cursor kc, vc[2];
+                kc.open(list, s.t0 * 8 + w, s.r.n_stale, P.tiles, 1);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int run = t * 8 + (w & ~1) + e;
-                        rec[e] = nullptr;
-                        if (t < n_tiles && run < s.r.n_stale) {
-                            const int pg = run / P.tiles, sub = run - pg * P.tiles;
-                            const int2 entry = list[pg];
-                            const uint8_t* page = base3 + (size_t)entry.y * P.hkv * page3;
-                            rec[e] = page + (size_t)sub * tq3_tile_bytes(D);
-                            meta[e] = page + (size_t)P.tiles * tq3_tile_bytes(D);
-                            pos[e] = (entry.x * P.tiles + sub) * kPage;
-                        }
-                    }
-                };
+                for (int e = 0; e < 2; ++e) vc[e].open(list, s.t0 * 8 + (w & ~1) + e, s.r.n_stale, P.tiles, 1);
                 uint32_t kw[LW], gw, vw[2][LW / 2 + (LW / 2 & 1)], mw[2][D / 32][2];
-                auto load_keys = [&] {
-                    const uint8_t* r = rec[half];
-                    if (!r) {
+                auto load_keys = [&] {                           // of the tile that kc is at, which moves on
+                    if (!kc.ok) {
 #pragma unroll
                         for (int i = 0; i < LW; ++i) kw[i] = 0;
                         gw = 0;
                         return;
                     }
+                    const uint8_t* r = base3 + (size_t)kc.entry.y * P.hkv * page3 + (size_t)kc.sub * tq3_tile_bytes(D);
 #pragma unroll
                     for (int c = 0; c < LW / 4; ++c) {
                         const uint4 v = ldg128(r + c * 512 + lane * 16);
@@ -715,22 +778,22 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                         const uint2 v = ldg64(r + (LW / 4) * 512 + lane * 8);
                         kw[LW - 2] = v.x; kw[LW - 1] = v.y;
                     }
-                    // g of tokens g and g + 8
-                    const __half* gp = reinterpret_cast<const __half*>(r + 12 * D);
-                    gw = (uint32_t)*reinterpret_cast<const volatile uint16_t*>(gp + g) |
-                         (uint32_t)*reinterpret_cast<const volatile uint16_t*>(gp + g + 8) << 16;
+                    gw = ldg16(r + 12 * D + 2 * g) | ldg16(r + 12 * D + 2 * g + 16) << 16;      // g of tokens g and g + 8
+                    kc.next();
                 };
                 auto load_values = [&] {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        if (!rec[e]) {
+                        if (!vc[e].ok) {
 #pragma unroll
                             for (int i = 0; i < (int)(sizeof vw[0] / 4); ++i) vw[e][i] = 0;
 #pragma unroll
                             for (int i = 0; i < D / 32; ++i) mw[e][i][0] = mw[e][i][1] = 0;
                             continue;
                         }
-                        const uint8_t* v = rec[e] + 6 * D;
+                        const uint8_t* page = base3 + (size_t)vc[e].entry.y * P.hkv * page3;
+                        const uint8_t* v = page + (size_t)vc[e].sub * tq3_tile_bytes(D) + 6 * D;
+                        const uint8_t* meta = page + (size_t)P.tiles * tq3_tile_bytes(D);
                         if constexpr (D == 256) {                // words 0-5 or 6-11 of the lane
                             if (half == 0) {
                                 const uint4 a = ldg128(v + lane * 16);
@@ -754,57 +817,60 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                         // scale / zero of the block pairs of these channels: (sc g, sc g+8), (zp g, zp g+8), twice
 #pragma unroll
                         for (int i = 0; i < D / 64; ++i) {
-                            const uint4 m = ldg128(meta[e] + (half * (D / 64) + i) * 128 + g * 16);
+                            const uint4 m = ldg128(meta + (half * (D / 64) + i) * 128 + g * 16);
                             mw[e][2 * i][0] = m.x; mw[e][2 * i][1] = m.y; mw[e][2 * i + 1][0] = m.z; mw[e][2 * i + 1][1] = m.w;
                         }
+                        vc[e].next();
                     }
                 };
-                locate(s.t0);
-                load_keys();
-                load_values();
-                fill_query(true);
-                for (int t = s.t0; t < n_tiles; ++t, ++tile) {
-                    const uint32_t st = tile % G::STAGES, ph = (tile / G::STAGES) & 1;
-                    if (tile >= G::STAGES) wait(kKEmpty + st, ph ^ 1);
+                auto put_keys = [&] {
+                    const uint32_t st = k_tile % G::STAGES;
+                    if (k_tile >= G::STAGES) wait(kKEmpty + st, (k_tile / G::STAGES & 1) ^ 1);
                     const uint32_t k_at = sb + G::OFF_K + st * G::K_TILE;
-                    {
-                        const int n0 = stale_row(w, g), n1 = stale_row(w, g + 8);
-                        const uint32_t g0 = hmul2_u32(prmt(gw, gw, 0x1010u), k_unit), g1 = hmul2_u32(prmt(gw, gw, 0x3232u), k_unit);
+                    const int n0 = stale_row(w, g), n1 = stale_row(w, g + 8);
+                    const uint32_t g0 = hmul2_u32(prmt(gw, gw, 0x1010u), k_unit), g1 = hmul2_u32(prmt(gw, gw, 0x3232u), k_unit);
 #pragma unroll
-                        for (int j = 0; j < D / 64; ++j) {
-                            const uint32_t A = kw[3 * j], Bw = kw[3 * j + 1], Cw = kw[3 * j + 2];
-                            uint32_t sel[4];
-                            sel[0] = A & 0x77777777u;
-                            sel[1] = Bw & 0x77777777u;
-                            sel[2] = lop3_and_or(A >> 1, 0x44444444u, Cw & 0x33333333u);
-                            sel[3] = lop3_and_or(Bw >> 1, 0x44444444u, (Cw >> 2) & 0x33333333u);
-                            const uint32_t at = k_at + j * (kKeys * 128);
+                    for (int j = 0; j < D / 64; ++j) {
+                        const uint32_t A = kw[3 * j], Bw = kw[3 * j + 1], Cw = kw[3 * j + 2];
+                        uint32_t sel[4];
+                        sel[0] = A & 0x77777777u;
+                        sel[1] = Bw & 0x77777777u;
+                        sel[2] = lop3_and_or(A >> 1, 0x44444444u, Cw & 0x33333333u);
+                        sel[3] = lop3_and_or(Bw >> 1, 0x44444444u, (Cw >> 2) & 0x33333333u);
+                        const uint32_t at = k_at + j * (kKeys * 128);
 #pragma unroll
-                            for (int c = 0; c < 2; ++c) {
-                                uint32_t lo[4], hi[4];           // chunk of token g, of token g + 8
-                                if constexpr (FMT == 2) {
-                                    key_lut4_v2(sel[2 * c], lo[0], lo[1]);
-                                    key_lut4_v2(sel[2 * c] >> 16, lo[2], lo[3]);
-                                    key_lut4_v2(sel[2 * c + 1], hi[0], hi[1]);
-                                    key_lut4_v2(sel[2 * c + 1] >> 16, hi[2], hi[3]);
-                                } else {
-                                    key_lut4(sel[2 * c], lo[0], hi[0]);
-                                    key_lut4(sel[2 * c] >> 16, lo[1], hi[1]);
-                                    key_lut4(sel[2 * c + 1], lo[2], hi[2]);
-                                    key_lut4(sel[2 * c + 1] >> 16, lo[3], hi[3]);
-                                }
-                                sts128(at + chunk_at(n0, 2 * tq + c), hmul2_u32(lo[0], g0), hmul2_u32(lo[1], g0), hmul2_u32(lo[2], g0), hmul2_u32(lo[3], g0));
-                                sts128(at + chunk_at(n1, 2 * tq + c), hmul2_u32(hi[0], g1), hmul2_u32(hi[1], g1), hmul2_u32(hi[2], g1), hmul2_u32(hi[3], g1));
+                        for (int c = 0; c < 2; ++c) {
+                            uint32_t lo[4], hi[4];               // chunk of token g, of token g + 8
+                            if constexpr (FMT == 2) {
+                                key_lut4_v2(sel[2 * c], lo[0], lo[1]);
+                                key_lut4_v2(sel[2 * c] >> 16, lo[2], lo[3]);
+                                key_lut4_v2(sel[2 * c + 1], hi[0], hi[1]);
+                                key_lut4_v2(sel[2 * c + 1] >> 16, hi[2], hi[3]);
+                            } else {
+                                key_lut4(sel[2 * c], lo[0], hi[0]);
+                                key_lut4(sel[2 * c] >> 16, lo[1], hi[1]);
+                                key_lut4(sel[2 * c + 1], lo[2], hi[2]);
+                                key_lut4(sel[2 * c + 1] >> 16, lo[3], hi[3]);
                             }
+                            sts128(at + chunk_at(n0, 2 * tq + c), hmul2_u32(lo[0], g0), hmul2_u32(lo[1], g0), hmul2_u32(lo[2], g0), hmul2_u32(lo[3], g0));
+                            sts128(at + chunk_at(n1, 2 * tq + c), hmul2_u32(hi[0], g1), hmul2_u32(hi[1], g1), hmul2_u32(hi[2], g1), hmul2_u32(hi[3], g1));
                         }
                     }
                     arrive(kKFull + st);
-                    const bool masked = t * 8 + 8 > s.r.n_stale || s.r.stale_end * kPage > first_pos + 1;
-                    const bool had[2] = {rec[0] != nullptr, rec[1] != nullptr};
-                    const int at_pos[2] = {pos[0], pos[1]};
-                    locate(t + 1);
-                    load_keys();
-                    if (tile >= G::STAGES) wait(kVEmpty + st, ph ^ 1);
+                    ++k_tile;
+                };
+                auto put_values = [&] {
+                    if (P.ve != 0) {
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+#pragma unroll
+                            for (int i = 0; i < D / 32; ++i) {
+                                mw[e][i][0] = hmul2_u32(mw[e][i][0], v_unit);
+                                mw[e][i][1] = hmul2_u32(mw[e][i][1], v_unit);
+                            }
+                    }
+                    const uint32_t st = v_tile % G::STAGES;
+                    if (v_tile >= G::STAGES) wait(kVEmpty + st, (v_tile / G::STAGES & 1) ^ 1);
                     const uint32_t v_at = sb + G::OFF_V + st * G::V_TILE + (w >> 2) * (D * 128);
                     const int c = 2 * tq + ((w >> 1) & 1);
 #pragma unroll
@@ -826,65 +892,67 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                                 else if (blk == 1) value_operands<1>(a, W0, W1, W2, X0[e]);
                                 else if (blk == 2) value_operands<2>(a, W0, W1, W2, X1[e]);
                                 else value_operands<3>(a, W0, W1, W2, X1[e]);
-                                const uint32_t sc = hmul2_u32(mw[e][4 * j + blk][0], v_unit), zp = hmul2_u32(mw[e][4 * j + blk][1], v_unit);
-                                const uint32_t s0 = prmt(sc, sc, 0x1010u), s1 = prmt(sc, sc, 0x3232u);
-                                const uint32_t z0 = prmt(zp, zp, 0x1010u), z1 = prmt(zp, zp, 0x3232u);
-                                o[e][0] = hfma2_u32(a[0], s0, z0);
-                                o[e][1] = hfma2_u32(a[2], s0, z0);
-                                o[e][2] = hfma2_u32(a[1], s1, z1);
-                                o[e][3] = hfma2_u32(a[3], s1, z1);
+                                const __half2 sc = as_half2(mw[e][4 * j + blk][0]), zp = as_half2(mw[e][4 * j + blk][1]);
+                                o[e][0] = as_u32(__hfma2(as_half2(a[0]), __low2half2(sc), __low2half2(zp)));
+                                o[e][1] = as_u32(__hfma2(as_half2(a[2]), __low2half2(sc), __low2half2(zp)));
+                                o[e][2] = as_u32(__hfma2(as_half2(a[1]), __high2half2(sc), __high2half2(zp)));
+                                o[e][3] = as_u32(__hfma2(as_half2(a[3]), __high2half2(sc), __high2half2(zp)));
                             }
                             const int ch = half * (D / 2) + 64 * j + 16 * blk + g;
-                            if (masked) {
-#pragma unroll
-                                for (int e = 0; e < 2; ++e)
-#pragma unroll
-                                    for (int i = 0; i < 4; ++i)
-                                        if (had[e] && has_nan2(o[e][i])) {         // a scale or zero that is not a number
-                                            note_nan(ch + 8 * (i >> 1), at_pos[e] + 2 * tq + 8 * (i & 1));
-                                            o[e][i] = 0;
-                                        }
-                            }
                             sts128(v_at + chunk_at(ch, c), o[0][0], o[0][1], o[1][0], o[1][1]);
                             sts128(v_at + chunk_at(ch + 8, c), o[0][2], o[0][3], o[1][2], o[1][3]);
                         }
                     }
                     arrive(kVFull + st);
+                    ++v_tile;
+                };
+                load_keys();
+                load_values();
+                fill_query(true);
+                put_keys();
+                load_keys();
+                for (int t = s.t0; t < n_tiles; ++t) {
+                    if (t + 1 < n_tiles) {
+                        put_keys();
+                        load_keys();
+                    }
+                    put_values();
                     load_values();
                 }
             }
             if (s.t1 > cut) {
                 // ---- FP8 tiles: a warp per run
                 constexpr int N = 16 * D / 512;                  // 16-byte loads of a lane for a run's keys, or values
-                const uint8_t* rec;
-                int pos;
-                auto locate = [&](int t) {
-                    const int run = (t - cut) * 8 + w;
-                    rec = nullptr;
-                    if (t < s.t1 && run < s.u.n_fp8) {
-                        const int pg = run / P.tiles, sub = run - pg * P.tiles;
-                        const int2 entry = list[P.max_pages - 1 - pg];
-                        rec = base8 + (size_t)entry.y * P.hkv * page8 + (size_t)sub * fp8_record_bytes(D);
-                        pos = (entry.x * P.tiles + sub) * kPage;
-                    }
-                };
-                uint4 kr[N], vr[N];
-                auto load = [&](uint4 (&x)[N], int off) {
-#pragma unroll
-                    for (int i = 0; i < N; ++i) x[i] = rec ? ldg128(rec + off + i * 512 + lane * 16) : make_uint4(0, 0, 0, 0);
-                };
                 const int t_first = max(s.t0, cut);
-                locate(t_first);
-                load(kr, 0);
-                load(vr, 16 * D);
-                fill_query(false);
-                for (int t = t_first; t < s.t1; ++t, ++tile) {
-                    const uint32_t st = tile % G::STAGES, ph = (tile / G::STAGES) & 1;
-                    if (tile >= G::STAGES) wait(kKEmpty + st, ph ^ 1);
+                Cursor kc, vc;
+                kc.open(list + P.max_pages - 1, (t_first - cut) * 8 + w, s.u.n_fp8, P.tiles, -1);
+                vc = kc;
+                uint4 kr[N], vr[N];
+                int v_pos = 0, left = 0;                         // of the run whose values are loaded: first position, tokens that exist
+                auto load = [&](uint4 (&x)[N], Cursor& c, int off) {
+                    const uint8_t* rec = base8 + (size_t)c.entry.y * P.hkv * page8 + (size_t)c.sub * fp8_record_bytes(D) + off;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) x[i] = c.ok ? ldg128(rec + i * 512) : make_uint4(0, 0, 0, 0);
+                };
+                // eight lanes take 64 dims of two keys: their 16-byte stores meet every bank once
+                const int k_tok = (D == 128 ? 2 * (lane >> 4) : 0) + ((lane >> 2) & 1), k_atom = D == 128 ? (lane >> 3) & 1 : lane >> 3;
+                auto load_keys = [&] {
+                    load(kr, kc, k_tok * D + k_atom * 64 + (lane & 3) * 16);
+                    kc.next();
+                };
+                auto load_values = [&] {
+                    load(vr, vc, 16 * D + lane * 16);
+                    v_pos = (vc.entry.x * P.tiles + vc.sub) * kPage;
+                    left = vc.ok ? s.r.len - v_pos : 0;
+                    vc.next();
+                };
+                auto put_keys = [&] {
+                    const uint32_t st = k_tile % G::STAGES;
+                    if (k_tile >= G::STAGES) wait(kKEmpty + st, (k_tile / G::STAGES & 1) ^ 1);
                     const uint32_t k_at = sb + G::OFF_K + st * G::K_TILE;
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
-                        const int off = i * 512 + lane * 16, tok = off / D, dim = off % D, row = 16 * w + tok;
+                        const int row = 16 * w + k_tok + i * (512 / D), c = 2 * (lane & 3);
                         const uint32_t x[4] = {kr[i].x, kr[i].y, kr[i].z, kr[i].w};
                         uint32_t o[8];
 #pragma unroll
@@ -892,68 +960,83 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                             o[2 * q] = e4m3x2_to_f16x2((uint16_t)(x[q] & 0xffffu));
                             o[2 * q + 1] = e4m3x2_to_f16x2((uint16_t)(x[q] >> 16));
                         }
-                        // chunks c, c + 1; of eight lanes of a row four store them in turned order (bank conflicts)
-                        const uint32_t at = k_at + (dim >> 6) * (kKeys * 128);
-                        const int c = (dim & 63) >> 3;
-                        const bool turn = lane & 4;
-                        sts128(at + chunk_at(row, turn ? c + 1 : c), turn ? o[4] : o[0], turn ? o[5] : o[1], turn ? o[6] : o[2], turn ? o[7] : o[3]);
-                        sts128(at + chunk_at(row, turn ? c : c + 1), turn ? o[0] : o[4], turn ? o[1] : o[5], turn ? o[2] : o[6], turn ? o[3] : o[7]);
+                        const uint32_t at = k_at + k_atom * (kKeys * 128);
+                        sts128(at + chunk_at(row, c), o[0], o[1], o[2], o[3]);
+                        sts128(at + chunk_at(row, c + 1), o[4], o[5], o[6], o[7]);
                     }
                     arrive(kKFull + st);
-                    const int left = rec ? s.r.len - pos : 0;    // tokens of the run that exist
-                    const int this_pos = pos;
-                    const bool masked = rec && pos + kPage - 1 > first_pos;
-                    locate(t + 1);
-                    load(kr, 0);
-                    if (tile >= G::STAGES) wait(kVEmpty + st, ph ^ 1);
+                    ++k_tile;
+                };
+                auto put_values = [&] {
+                    const uint32_t st = v_tile % G::STAGES;
+                    if (v_tile >= G::STAGES) wait(kVEmpty + st, (v_tile / G::STAGES & 1) ^ 1);
+                    if (left < kPage) {                          // what no token fills may be anything
+#pragma unroll
+                        for (int i = 0; i < N; ++i) {
+                            uint32_t* word = reinterpret_cast<uint32_t*>(&vr[i]);
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                const int keep = left - 4 * q;
+                                word[q] &= keep >= 4 ? FULL : keep <= 0 ? 0u : (1u << (8 * keep)) - 1u;
+                            }
+                        }
+                    }
+                    if (left > 0 && v_pos + kPage - 1 > first_pos) {                  // some row does not see the whole run
+                        uint32_t bad = 0;
+#pragma unroll
+                        for (int i = 0; i < N; ++i) {
+                            const uint32_t x[4] = {vr[i].x, vr[i].y, vr[i].z, vr[i].w};
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) bad |= __vcmpeq4(x[q] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+                        }
+                        if (bad) note_nan(vr, v_pos);
+                        __syncwarp();
+                    }
                     const uint32_t v_at = sb + G::OFF_V + st * G::V_TILE + (w >> 2) * (D * 128);
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
                         const int ch = i * 32 + lane, c = 2 * (w & 3);
-                        uint32_t x[4] = {vr[i].x, vr[i].y, vr[i].z, vr[i].w};
-                        if (left < kPage) {                      // what no token fills may be anything
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                const int keep = left - 4 * q;
-                                x[q] &= keep >= 4 ? FULL : keep <= 0 ? 0u : (1u << (8 * keep)) - 1u;
-                            }
-                        }
+                        const uint32_t x[4] = {vr[i].x, vr[i].y, vr[i].z, vr[i].w};
                         uint32_t o[8];
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
                             o[2 * q] = e4m3x2_to_f16x2((uint16_t)(x[q] & 0xffffu));
                             o[2 * q + 1] = e4m3x2_to_f16x2((uint16_t)(x[q] >> 16));
                         }
-                        if (masked) {
-#pragma unroll
-                            for (int q = 0; q < 8; ++q)
-                                if (has_nan2(o[q])) {
-                                    const __half2 h = *reinterpret_cast<const __half2*>(&o[q]);
-                                    const bool low = __hisnan(__low2half(h));
-                                    note_nan(ch, this_pos + 2 * q + (low ? 0 : 1));
-                                    o[q] &= (low ? 0xffff0000u : FULL) & (__hisnan(__high2half(h)) ? 0x0000ffffu : FULL);
-                                }
-                        }
                         sts128(v_at + chunk_at(ch, c), o[0], o[1], o[2], o[3]);
                         sts128(v_at + chunk_at(ch, c + 1), o[4], o[5], o[6], o[7]);
                     }
                     arrive(kVFull + st);
-                    load(vr, 16 * D);
+                    ++v_tile;
+                };
+                load_keys();
+                load_values();
+                fill_query(false);
+                put_keys();
+                load_keys();
+                for (int t = t_first; t < s.t1; ++t) {
+                    if (t + 1 < s.t1) {
+                        put_keys();
+                        load_keys();
+                    }
+                    put_values();
+                    load_values();
                 }
             }
         }
     } else {
         // ================= softmax and output =================
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(G::SOFT_REGS));
         const int t = warp >> 2;                                 // row tile
         const uint32_t my_lanes = (uint32_t)(32 * (warp & 3)) << 16;
         const int my_row = t * 128 + (warp & 3) * 32 + lane;     // within the unit
         const uint32_t col_o = tb + my_lanes + t * D;
-        uint32_t job = 0, fills = 0, done = 0, segments = 0;     // done: products with the values so far on this row tile
+        uint32_t job = 0, fills = 0, done = 0, outputs = 0, segments = 0;   // done, outputs: value products, segments with any, on this row tile
         auto warp_arrive = [&](int i) {
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(i));
         };
-        while (walk.next(s)) {
+        while (walk.next(P, share, s)) {
             ++segments;
             const int row = s.rt * ROWS + my_row, n_rows = s.r.n_new * P.group;
             const bool live = row < n_rows, warp_live = row - lane < n_rows;
@@ -984,38 +1067,46 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                     const int n_in = min(8, (stale ? s.r.n_stale : s.u.n_fp8) - (stale ? kt : kt - cut) * 8);
                     bool masked = n_in < 8 || !ordinary;
                     if (!masked && !stale) masked = (runs - s.r.n_fp8 + (kt - cut) * 8 + 7) * kPage + kPage - 1 > first_pos;
-                    int seen[8];                                 // tokens of run e that the row sees, from its first one
-                    if (masked) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            seen[e] = 0;
-                            if (e < n_in) {
-                                const int run = (stale ? kt : kt - cut) * 8 + e, pg = run / P.tiles, sub = run - pg * P.tiles;
-                                const int lp = list[stale ? pg : P.max_pages - 1 - pg].x;
-                                seen[e] = qpos - (lp * P.tiles + sub) * kPage + 1;
-                            }
-                        }
-                    }
-                    auto hide = [&](float (&x)[32], int c0) {
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) {
-                            const int n = c0 + c;
-                            const bool out = stale ? token_of_row(n) >= seen[run_of_row(n)] : (n & 15) >= seen[n >> 4];
-                            if (out) x[c] = -CUDART_INF_F;
-                        }
-                    };
-                    float mx = -CUDART_INF_F;
-                    {
-                        float x[32];
-#pragma unroll
+                    if (masked) {                                // what the row does not see becomes -inf in tensor memory
+#pragma unroll 1
                         for (int c = 0; c < 4; ++c) {
-                            tmem_ld32(col_s + 32 * c, x);
-                            tmem_wait_ld();
-                            if (masked) hide(x, 32 * c);
+                            int seen[4];                         // tokens that the row sees of the runs in these 32 columns
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) mx = fmaxf(mx, x[k]);
+                            for (int k = 0; k < 4; ++k) {
+                                const int e = stale ? 4 * (c >> 1) + k : 2 * c + (k & 1);
+                                seen[k] = 0;
+                                if (e < n_in) {
+                                    const int run = (stale ? kt : kt - cut) * 8 + e, pg = run / P.tiles, sub = run - pg * P.tiles;
+                                    const int lp = list[stale ? pg : P.max_pages - 1 - pg].x;
+                                    seen[k] = qpos - (lp * P.tiles + sub) * kPage + 1;
+                                }
+                            }
+                            float x[32];
+                            tmem_ld32(col_s + 32 * c, x);
+                            tmem_wait_ld32(x);
+                            const int t_add = 4 * (c & 1);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) {
+                                const int lim = stale ? seen[2 * ((k >> 3) & 1) + ((k >> 2) & 1)] : seen[k >> 4];
+                                const int tk = stale ? t_add + 2 * (k >> 4) + (k & 1) + 8 * ((k >> 1) & 1) : k & 15;
+                                if (tk >= lim) x[k] = -CUDART_INF_F;
+                            }
+                            tmem_st32(col_s + 32 * c, x);
                         }
-                        mx *= fac;
+                        tmem_wait_st();
+                    }
+                    float mx;
+                    {
+                        float m4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            float x[32];
+                            tmem_ld32(col_s + 32 * c, x);
+                            tmem_wait_ld32(x);
+#pragma unroll
+                            for (int k = 0; k < 32; k += 2) m4[(k >> 1) & 3] = fmaxf(m4[(k >> 1) & 3], fmaxf(x[k], x[k + 1]));
+                        }
+                        mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * fac;
                     }
                     const bool raise = mx > ref + (kShift + kSlack);
                     if (__any_sync(FULL, raise) || turn) {
@@ -1025,13 +1116,14 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                         sum *= f;
                         if (n_done > 0) {
                             const float fo = turn ? f * (__uint_as_float((uint32_t)(127 + P.ve) << 23) / P.v_scale) : f;
+                            // the product before that one is done (these scores were issued behind it), so the parity is this one's
                             wait(kPvDone + t, (done - 1) & 1);
                             tc_fence_after();
                             float x[32];
 #pragma unroll 1
                             for (int c = 0; c < D / 32; ++c) {
                                 tmem_ld32(col_o + 32 * c, x);
-                                tmem_wait_ld();
+                                tmem_wait_ld32(x);
 #pragma unroll
                                 for (int k = 0; k < 32; ++k) x[k] *= fo;
                                 tmem_st32(col_o + 32 * c, x);
@@ -1039,13 +1131,12 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                         }
                     }
                     const float base = ref == -CUDART_INF_F ? 0.f : ref;
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < 4; ++c) {
                         float x[32];
                         uint32_t h2[16];
                         tmem_ld32(col_s + 32 * c, x);
-                        tmem_wait_ld();
-                        if (masked) hide(x, 32 * c);
+                        tmem_wait_ld32(x);
                         float s0 = 0.f, s1 = 0.f;
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
@@ -1065,14 +1156,15 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                 ++n_done;
             }
             job += (uint32_t)(s.t1 - s.t0) * s.nt;
+            if (n_done > 0) ++outputs;
             if (t < s.nt && warp_live) {
                 if (n_done > 0) {
-                    wait(kPvDone + t, (done - 1) & 1);
+                    wait(kOutput + t, (outputs - 1) & 1);
                     tc_fence_after();
                 }
                 // accumulators are in units of the last tile's values
                 const float unit = s.t1 > cut ? P.v_scale : __uint_as_float((uint32_t)(127 + P.ve) << 23);
-                const bool none = sum == 0.f;
+                const bool none = sum == 0.f, noted = *noted_s == segments;
                 const float f = s.slot >= 0 ? unit : none ? 0.f : unit / sum;
                 const size_t orow = (size_t)(s.r.row0 + tok) * (P.hkv * P.group) + head;
                 const size_t prow = (size_t)max(s.slot, 0) * ROWS + my_row;
@@ -1081,13 +1173,16 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                     float x[32];
                     if (n_done > 0) {
                         tmem_ld32(col_o + 32 * c, x);
-                        tmem_wait_ld();
+                        tmem_wait_ld32(x);
                     }
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        x[k] = none || n_done == 0 ? 0.f : x[k] * f;
-                        const unsigned long long note = nan_s[32 * c + k];
-                        if ((uint32_t)(note >> 32) == segments && kNoPos - (int)(uint32_t)note <= qpos) x[k] = CUDART_NAN_F;
+                    for (int k = 0; k < 32; ++k) x[k] = none || n_done == 0 ? 0.f : x[k] * f;
+                    if (noted) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) {
+                            const unsigned long long note = nan_s[32 * c + k];
+                            if ((uint32_t)(note >> 32) == segments && kNoPos - (int)(uint32_t)note <= qpos) x[k] = CUDART_NAN_F;
+                        }
                     }
                     if (!live) continue;
                     if (s.slot >= 0) {
@@ -1197,6 +1292,13 @@ template <int D, int FMT>
 static int32_t launch(const Params& P, int sms, cudaStream_t s)
 {
     using G = Geo<D>;
+    // the warps' shares of the registers add up to the launch's: a build that takes fewer would wait for the rest for ever
+    cudaFuncAttributes attr;
+    MKV_CUDA(cudaFuncGetAttributes(&attr, chunk_scan_kernel<D, FMT>));
+    if (attr.numRegs != G::REGS) {
+        set_last_error("chunk attention: the kernel was built with another number of registers than its warps share out");
+        return MKV_E_CUDA;
+    }
     MKV_CUDA(cudaFuncSetAttribute(chunk_scan_kernel<D, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM));
     const int blocks = sms < kMaxBlocks ? sms : kMaxBlocks;
     MKV_CUDA(launch_pdl(chunk_plan_kernel<G::ROWS>, dim3(P.B), kPlanThreads, 0, 1, s, P));
