@@ -39,6 +39,7 @@ constexpr int kUnitCost = 2;                 // what a unit costs besides its ke
 constexpr int kLeastShare = 3;               // key tiles of a block at least
 constexpr float kShift = 7.f, kSlack = 8.f;  // see above: probabilities are at most 2^(kShift + kSlack)
 constexpr int kNoPos = 0x7fffffff;
+constexpr uint32_t kHoldNs = 10000;          // of one poll of a barrier
 
 // What chunk_plan_kernel leaves of a request.  Runs are of 16 tokens.
 struct Request {
@@ -315,11 +316,27 @@ __device__ __forceinline__ void sts64(uint32_t addr, uint32_t a, uint32_t b)
 }
 __device__ __forceinline__ void sts32(uint32_t addr, uint32_t a) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(a) : "memory"); }
 
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate)
+// Products are issued by a whole warp in step, one elected lane of it taking effect: descriptors and addresses then live in
+// uniform registers.  (Issued from a lane's own branch every operand is moved there first, 190 cycles a product.)
+__device__ __forceinline__ void issue_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate)
 {
-    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+    asm volatile("{\n .reg .pred p, e;\n elect.sync _|e, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n"
+                 " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
                  ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
 }
+__device__ __forceinline__ void issue_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate)
+{
+    asm volatile("{\n .reg .pred p, e;\n elect.sync _|e, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n"
+                 " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void issue_commit(uint32_t bar)
+{
+    asm volatile("{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n"
+                 " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar) : "memory");
+}
+// a value that is the same in every lane, in a uniform register
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_max_sync(0xffffffffu, x); }
 // 32 columns of the thread's tensor-memory lane
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&r)[32])
 {
@@ -330,16 +347,6 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&r)[32])
                    "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]),
                    "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
                  : "r"(taddr) : "memory");
-}
-// waits for the loads so far; the values pass through, so that nothing computed from them is moved before the wait
-__device__ __forceinline__ void tmem_wait_ld32(float (&r)[32])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]), "+f"(r[8]),
-                   "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]), "+f"(r[16]),
-                   "+f"(r[17]), "+f"(r[18]), "+f"(r[19]), "+f"(r[20]), "+f"(r[21]), "+f"(r[22]), "+f"(r[23]), "+f"(r[24]),
-                   "+f"(r[25]), "+f"(r[26]), "+f"(r[27]), "+f"(r[28]) :: "memory");
-    asm volatile("" : "+f"(r[29]), "+f"(r[30]), "+f"(r[31]) :: "memory");
 }
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&r)[32])
 {
@@ -355,6 +362,21 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
                  ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
                    "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+// two fp32 operations in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(reinterpret_cast<unsigned long long&>(r))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)), "l"(reinterpret_cast<unsigned long long&>(c)));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<unsigned long long&>(r))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+    return r;
 }
 __device__ __forceinline__ uint32_t hmul2_u32(uint32_t a, uint32_t b)
 {
@@ -454,11 +476,11 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
     constexpr int NT = G::NT, ROWS = G::ROWS;
     constexpr uint32_t FULL = 0xffffffffu;
     extern __shared__ uint8_t smem_raw[];
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    const uint32_t sb = smem_u32(smem);
+    const uint32_t raw_at = smem_u32(smem_raw), sb = (raw_at + 1023) & ~1023u;
+    uint8_t* smem = smem_raw + (sb - raw_at);
     float* fac_s = reinterpret_cast<float*>(smem + G::OFF_FAC);
     unsigned long long* nan_s = reinterpret_cast<unsigned long long*>(smem + G::OFF_NAN);
-    volatile int* failed_s = reinterpret_cast<volatile int*>(smem + G::OFF_MISC);
+    const uint32_t failed_at = sb + G::OFF_MISC;                 // word: a wait has given up
     uint32_t* tmem_s = reinterpret_cast<uint32_t*>(smem + G::OFF_MISC + 4);
     volatile uint32_t* noted_s = reinterpret_cast<volatile uint32_t*>(smem + G::OFF_MISC + 8);    // segment of the latest note
     Share* share = reinterpret_cast<Share*>(smem + G::OFF_MISC + 16);
@@ -473,7 +495,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
             else if (i == kFacRead || i == kSegDone) count = G::SOFT_WARPS;
             mbar_init(bar(i), count);
         }
-        *failed_s = 0;
+        sts32(failed_at, 0);
         *noted_s = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -526,20 +548,19 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
     Walker<ROWS> walk(P, share);
     Segment s;
 
-    // bounded by wall time: a wait that gives up flags the pool and lets every later wait of the block pass
+    // Bounded by wall time: a wait that gives up flags the pool and lets every later wait of the block pass.  The hardware
+    // holds a waiting warp back for a while, so that its polling does not take the working warps' issue slots.
     auto wait = [&](int i, uint32_t parity) {
         const uint32_t a = bar(i);
-        if (mbar_try_wait(a, parity)) return;
-        unsigned long long t0 = 0, t1;
-        for (int spins = 1; !*failed_s; ++spins) {
-            if (mbar_try_wait(a, parity)) return;
-            if ((spins & 63) == 0) {
-                asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));
-                if (t0 == 0) t0 = t1;
-                if (t1 - t0 > P.wait_ns) {
-                    *failed_s = 1;
-                    atomicOr(P.status, kStTimeout);
-                }
+        if (mbar_try_wait_hint(a, parity, kHoldNs)) return;
+        unsigned long long t0, t1;
+        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+        while (!mbar_try_wait_hint(a, parity, kHoldNs)) {
+            if (lds32(failed_at)) return;
+            asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));
+            if (t1 - t0 > P.wait_ns) {
+                sts32(failed_at, 1);
+                atomicOr(P.status, kStTimeout);
             }
         }
     };
@@ -547,55 +568,52 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
     if (warp >= G::MMA_WARP) {
         // ================= products =================
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(G::MMA_REGS));
-        if (warp == G::MMA_WARP && lane == 0) {
+        if (warp == G::MMA_WARP) {
+            constexpr uint32_t kTb = 0;                          // the whole of tensor memory is this block's
             uint32_t job = 0, tile = 0, fills = 0;               // scores, key tiles and queries so far
             while (walk.next(P, share, s)) {
-                const int n = (s.t1 - s.t0) * s.nt, cut = s.u.stale_tiles;
+                const int nt = (int)uniform(s.nt), n = (int)uniform(s.t1 - s.t0) * nt, cut = s.u.stale_tiles;
                 // job i of the segment: key tile t0 + i / nt, row tile i % nt; its scores are issued two jobs ahead
                 for (int i = -2; i < n; ++i) {
                     if (i >= 0) {
-                        const int j = s.nt == 2 ? i >> 1 : i, t = s.nt == 2 ? i & 1 : 0;
-                        const uint32_t at = tile + j, st = at % G::STAGES, buf = (job + i) & 1;
+                        const uint32_t j = nt == 2 ? i >> 1 : i, t = nt == 2 ? i & 1 : 0;
+                        const uint32_t at = uniform(tile) + j, st = at % G::STAGES, buf = (uniform(job) + i) & 1;
                         if (t == 0) wait(kVFull + st, (at / G::STAGES) & 1);
                         wait(kPFull + buf, ((job + i) >> 1) & 1);
                         tc_fence_after();
                         const uint64_t v = operand_desc(sb + G::OFF_V + st * G::V_TILE);
-                        const uint32_t o = tb + t * D, p = tb + kColS + kKeys * buf;
-#pragma unroll 1
-                        for (int half = 0; half < 2; ++half)
+                        const uint32_t o = kTb + t * D, p = kTb + kColS + kKeys * buf;
 #pragma unroll
-                            for (int kk = 0; kk < 4; ++kk)
-                                mma_ts(o, p + 32 * half + 8 * kk, v + ((half * (D * 128) + kk * 32) >> 4), idesc(D), j > 0 || half > 0 || kk > 0);
-                        mma_commit(bar(kPvDone + t));
-                        if (i + s.nt >= n) mma_commit(bar(kOutput + t));
-                        if (t == s.nt - 1) mma_commit(bar(kVEmpty + st));
+                        for (int kk = 0; kk < kKeys / 16; ++kk)
+                            issue_ts(o, p + 8 * kk, v + (((kk >> 2) * (D * 128) + (kk & 3) * 32) >> 4), idesc(D), kk > 0 ? 1u : (j > 0 ? 1u : 0u));
+                        issue_commit(bar(kPvDone + t));
+                        if (i + nt >= n) issue_commit(bar(kOutput + t));
+                        if ((int)t == nt - 1) issue_commit(bar(kVEmpty + st));
                     }
                     if (i + 2 < n) {
-                        const int i2 = i + 2, j = s.nt == 2 ? i2 >> 1 : i2, t = s.nt == 2 ? i2 & 1 : 0;
-                        const uint32_t at = tile + j, st = at % G::STAGES, buf = (job + i2) & 1;
+                        const uint32_t i2 = i + 2, j = nt == 2 ? i2 >> 1 : i2, t = nt == 2 ? i2 & 1 : 0;
+                        const uint32_t at = uniform(tile) + j, st = at % G::STAGES, buf = (uniform(job) + i2) & 1;
                         if (t == 0) {
-                            if (j == 0 || s.t0 + j == cut) wait(kQFull, fills++ & 1);
+                            if (j == 0 || s.t0 + (int)j == cut) wait(kQFull, fills++ & 1);
                             wait(kKFull + st, (at / G::STAGES) & 1);
                             tc_fence_after();
                         }
                         const uint64_t a = operand_desc(sb + G::OFF_Q + t * G::Q_TILE), k = operand_desc(sb + G::OFF_K + st * G::K_TILE);
-                        const uint32_t d = tb + kColS + kKeys * buf;
-#pragma unroll 1
-                        for (int atom = 0; atom < D / 64; ++atom)
+                        const uint32_t d = kTb + kColS + kKeys * buf;
 #pragma unroll
-                            for (int kk = 0; kk < 4; ++kk) {
-                                const uint64_t step = (atom * (128 * 128) + kk * 32) >> 4;
-                                mma_ss(d, a + step, k + step, idesc(kKeys), atom > 0 || kk > 0);
-                            }
-                        mma_commit(bar(kSFull + buf));
-                        if (t == s.nt - 1) mma_commit(bar(kKEmpty + st));
+                        for (int kk = 0; kk < D / 16; ++kk) {
+                            const uint64_t step = ((kk >> 2) * (128 * 128) + (kk & 3) * 32) >> 4;
+                            issue_ss(d, a + step, k + step, idesc(kKeys), kk > 0);
+                        }
+                        issue_commit(bar(kSFull + buf));
+                        if ((int)t == nt - 1) issue_commit(bar(kKEmpty + st));
                     }
                 }
                 job += n;
                 tile += s.t1 - s.t0;
             }
             // tensor memory is given back when nothing writes it any more (also after a wait that gave up; bounded again)
-            mma_commit(bar(kDrained));
+            issue_commit(bar(kDrained));
             unsigned long long t0, t1;
             asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
             while (!mbar_try_wait(bar(kDrained), 0)) {
@@ -1083,7 +1101,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                             }
                             float x[32];
                             tmem_ld32(col_s + 32 * c, x);
-                            tmem_wait_ld32(x);
+                            tmem_wait_ld();
                             const int t_add = 4 * (c & 1);
 #pragma unroll
                             for (int k = 0; k < 32; ++k) {
@@ -1102,7 +1120,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                         for (int c = 0; c < 4; ++c) {
                             float x[32];
                             tmem_ld32(col_s + 32 * c, x);
-                            tmem_wait_ld32(x);
+                            tmem_wait_ld();
 #pragma unroll
                             for (int k = 0; k < 32; k += 2) m4[(k >> 1) & 3] = fmaxf(m4[(k >> 1) & 3], fmaxf(x[k], x[k + 1]));
                         }
@@ -1123,7 +1141,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
 #pragma unroll 1
                             for (int c = 0; c < D / 32; ++c) {
                                 tmem_ld32(col_o + 32 * c, x);
-                                tmem_wait_ld32(x);
+                                tmem_wait_ld();
 #pragma unroll
                                 for (int k = 0; k < 32; ++k) x[k] *= fo;
                                 tmem_st32(col_o + 32 * c, x);
@@ -1136,16 +1154,17 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                         float x[32];
                         uint32_t h2[16];
                         tmem_ld32(col_s + 32 * c, x);
-                        tmem_wait_ld32(x);
-                        float s0 = 0.f, s1 = 0.f;
+                        tmem_wait_ld();
+                        float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
-                            const float a = fast_exp2(fmaf(x[2 * k], fac, -base)), d = fast_exp2(fmaf(x[2 * k + 1], fac, -base));
-                            s0 += a;
-                            s1 += d;
-                            h2[k] = pack_f16x2(a, d);
+                            float2 e = fma2(make_float2(x[2 * k], x[2 * k + 1]), make_float2(fac, fac), make_float2(-base, -base));
+                            e.x = fast_exp2(e.x);
+                            e.y = fast_exp2(e.y);
+                            s2 = add2(s2, e);
+                            h2[k] = pack_f16x2(e.x, e.y);
                         }
-                        sum += s0 + s1;
+                        sum += s2.x + s2.y;
                         tmem_st16(col_s + 16 * c, h2);
                     }
                     tmem_wait_st();
@@ -1173,7 +1192,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                     float x[32];
                     if (n_done > 0) {
                         tmem_ld32(col_o + 32 * c, x);
-                        tmem_wait_ld32(x);
+                        tmem_wait_ld();
                     }
 #pragma unroll
                     for (int k = 0; k < 32; ++k) x[k] = none || n_done == 0 ? 0.f : x[k] * f;
