@@ -39,7 +39,6 @@ constexpr int kUnitCost = 2;                 // what a unit costs besides its ke
 constexpr int kLeastShare = 3;               // key tiles of a block at least
 constexpr float kShift = 7.f, kSlack = 8.f;  // see above: probabilities are at most 2^(kShift + kSlack)
 constexpr int kNoPos = 0x7fffffff;
-constexpr uint32_t kHoldNs = 10000;          // of one poll of a barrier
 
 // What chunk_plan_kernel leaves of a request.  Runs are of 16 tokens.
 struct Request {
@@ -484,7 +483,8 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
     uint32_t* tmem_s = reinterpret_cast<uint32_t*>(smem + G::OFF_MISC + 4);
     volatile uint32_t* noted_s = reinterpret_cast<volatile uint32_t*>(smem + G::OFF_MISC + 8);    // segment of the latest note
     Share* share = reinterpret_cast<Share*>(smem + G::OFF_MISC + 16);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    // (the warp's number as a uniform value: whole-warp branches are then known as such)
+    const int tid = threadIdx.x, warp = (int)uniform((uint32_t)tid >> 5), lane = tid & 31;
     auto bar = [&](int i) -> uint32_t { return sb + G::OFF_BAR + 8 * i; };
 
     if (tid == 0) {
@@ -548,16 +548,18 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
     Walker<ROWS> walk(P, share);
     Segment s;
 
-    // Bounded by wall time: a wait that gives up flags the pool and lets every later wait of the block pass.  The hardware
-    // holds a waiting warp back for a while, so that its polling does not take the working warps' issue slots.
+    // Bounded by wall time: a wait that gives up flags the pool and lets every later wait of the block pass.  Polls are few
+    // instructions, since they take issue slots from the working warps.
     auto wait = [&](int i, uint32_t parity) {
         const uint32_t a = bar(i);
-        if (mbar_try_wait_hint(a, parity, kHoldNs)) return;
-        unsigned long long t0, t1;
-        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
-        while (!mbar_try_wait_hint(a, parity, kHoldNs)) {
+        if (mbar_try_wait(a, parity)) return;
+        unsigned long long t0 = 0, t1;
+        for (int polls = 1; !mbar_try_wait(a, parity); ++polls) {
+            __nanosleep(20);
+            if (polls & 63) continue;
             if (lds32(failed_at)) return;
             asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));
+            if (t0 == 0) t0 = t1;
             if (t1 - t0 > P.wait_ns) {
                 sts32(failed_at, 1);
                 atomicOr(P.status, kStTimeout);
@@ -571,13 +573,14 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
         if (warp == G::MMA_WARP) {
             constexpr uint32_t kTb = 0;                          // the whole of tensor memory is this block's
             uint32_t job = 0, tile = 0, fills = 0;               // scores, key tiles and queries so far
-            while (walk.next(P, share, s)) {
-                const int nt = (int)uniform(s.nt), n = (int)uniform(s.t1 - s.t0) * nt, cut = s.u.stale_tiles;
+            while (uniform(walk.next(P, share, s))) {
+                const int nt = (int)uniform(s.nt), n = (int)uniform(s.t1 - s.t0) * nt;
+                const int turn = (int)uniform(max(s.u.stale_tiles - s.t0, 0));        // key tile of the segment that starts the FP8 ones
                 // job i of the segment: key tile t0 + i / nt, row tile i % nt; its scores are issued two jobs ahead
                 for (int i = -2; i < n; ++i) {
                     if (i >= 0) {
                         const uint32_t j = nt == 2 ? i >> 1 : i, t = nt == 2 ? i & 1 : 0;
-                        const uint32_t at = uniform(tile) + j, st = at % G::STAGES, buf = (uniform(job) + i) & 1;
+                        const uint32_t at = tile + j, st = at % G::STAGES, buf = (job + i) & 1;
                         if (t == 0) wait(kVFull + st, (at / G::STAGES) & 1);
                         wait(kPFull + buf, ((job + i) >> 1) & 1);
                         tc_fence_after();
@@ -592,9 +595,9 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                     }
                     if (i + 2 < n) {
                         const uint32_t i2 = i + 2, j = nt == 2 ? i2 >> 1 : i2, t = nt == 2 ? i2 & 1 : 0;
-                        const uint32_t at = uniform(tile) + j, st = at % G::STAGES, buf = (uniform(job) + i2) & 1;
+                        const uint32_t at = tile + j, st = at % G::STAGES, buf = (job + i2) & 1;
                         if (t == 0) {
-                            if (j == 0 || s.t0 + (int)j == cut) wait(kQFull, fills++ & 1);
+                            if (j == 0 || (int)j == turn) wait(kQFull, fills++ & 1);
                             wait(kKFull + st, (at / G::STAGES) & 1);
                             tc_fence_after();
                         }
@@ -609,8 +612,8 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                         if ((int)t == nt - 1) issue_commit(bar(kKEmpty + st));
                     }
                 }
-                job += n;
-                tile += s.t1 - s.t0;
+                job = uniform(job + n);
+                tile = uniform(tile + n / nt);
             }
             // tensor memory is given back when nothing writes it any more (also after a wait that gave up; bounded again)
             issue_commit(bar(kDrained));
@@ -1149,6 +1152,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                         }
                     }
                     const float base = ref == -CUDART_INF_F ? 0.f : ref;
+                    const float2 fac2 = make_float2(fac, fac), base2 = make_float2(-base, -base);
 #pragma unroll 1
                     for (int c = 0; c < 4; ++c) {
                         float x[32];
@@ -1158,7 +1162,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                         float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
-                            float2 e = fma2(make_float2(x[2 * k], x[2 * k + 1]), make_float2(fac, fac), make_float2(-base, -base));
+                            float2 e = fma2(make_float2(x[2 * k], x[2 * k + 1]), fac2, base2);
                             e.x = fast_exp2(e.x);
                             e.y = fast_exp2(e.y);
                             s2 = add2(s2, e);
