@@ -40,6 +40,9 @@ constexpr int kLeastShare = 3;               // key tiles of a block at least
 constexpr float kShift = 7.f, kSlack = 8.f;  // see above: probabilities are at most 2^(kShift + kSlack)
 constexpr int kNoPos = 0x7fffffff;
 
+template <int N>
+struct Int { static constexpr int value = N; };
+
 // What chunk_plan_kernel leaves of a request.  Runs are of 16 tokens.
 struct Request {
     int n_new, row0, len;
@@ -77,27 +80,6 @@ struct Params {
     Merge* merge;
     uint32_t* status;
     unsigned long long wait_ns;
-};
-
-template <int D>
-struct Geo {
-    static constexpr int NT = D == 128 ? 2 : 1;                 // row tiles of a block
-    static constexpr int ROWS = 128 * NT;
-    static constexpr int STAGES = D == 128 ? 2 : 1;             // key tiles, and value tiles, in shared memory
-    static constexpr int Q_TILE = 128 * D * 2, K_TILE = kKeys * D * 2, V_TILE = K_TILE;
-    static constexpr int SOFT_WARPS = 4 * NT, UNPACK_WARPS = 8;
-    static constexpr int MMA_WARP = SOFT_WARPS + UNPACK_WARPS, THREADS = 32 * (MMA_WARP + 4);
-    // registers: of the launch, and of the softmax, unpacking and product warps afterwards (the sums agree)
-    static constexpr int REGS = D == 128 ? 96 : 128;
-    static constexpr int SOFT_REGS = D == 128 ? 104 : 144, UNPACK_REGS = D == 128 ? 104 : 144, MMA_REGS = D == 128 ? 64 : 80;
-    static_assert(SOFT_WARPS * SOFT_REGS + UNPACK_WARPS * UNPACK_REGS + 4 * MMA_REGS <= (MMA_WARP + 4) * REGS, "register split");
-    static constexpr int OFF_Q = 0, OFF_K = OFF_Q + NT * Q_TILE, OFF_V = OFF_K + STAGES * K_TILE;
-    static constexpr int OFF_FAC = OFF_V + STAGES * V_TILE;     // factor of every row's scores
-    static constexpr int OFF_NAN = OFF_FAC + ROWS * 4;          // 64-bit word per channel, see note_nan
-    static constexpr int OFF_BAR = OFF_NAN + D * 8;
-    static constexpr int OFF_MISC = OFF_BAR + 256;
-    static constexpr int SMEM = OFF_MISC + 128 + 1024;           // the tiles start on a 1,024-byte boundary
-    static_assert(SMEM <= 232448, "shared memory of a block");
 };
 
 // mbarriers (index); phases are counted by the waiting side
@@ -145,19 +127,23 @@ struct Share {
     int request;
 };
 
-// Walks the units that a block's share meets; every thread of a block does so by itself.
-template <int ROWS>
-struct Walker {
+// Walks the units that a block's share meets; every warp does so by itself, with its place and its present segment in shared
+// memory (registers are what the roles are short of).
+struct Walk {
+    Segment s;
     long long at;
     int b, h, rt;
 
-    __device__ __forceinline__ Walker(const Params& P, const Share* share) : at(share->request_start), b(share->request), h(0), rt(0)
+    __device__ __forceinline__ void open(const Params& P, const Share* share)
     {
-        const long long cost = P.req[b].cost, skip = (share->p0 - at) / cost;       // KV heads before the first unit
+        b = share->request;
+        rt = 0;
+        const long long cost = P.req[b].cost, skip = (share->p0 - share->request_start) / cost;      // KV heads before the first unit
         h = (int)skip;
-        at += skip * cost;
+        at = share->request_start + skip * cost;
     }
-    __device__ __forceinline__ bool next(const Params& P, const Share* share, Segment& s)
+    template <int ROWS>
+    __device__ __forceinline__ bool next(const Params& P, const Share* share)
     {
         const long long p0 = share->p0, p1 = share->p1;
         while (at < p1 && b < P.B) {
@@ -193,6 +179,29 @@ struct Walker {
         }
         return false;
     }
+};
+
+template <int D>
+struct Geo {
+    static constexpr int NT = D == 128 ? 2 : 1;                 // row tiles of a block
+    static constexpr int ROWS = 128 * NT;
+    static constexpr int COLS = 32;                             // score columns of a softmax step (registers)
+    static constexpr int STAGES = D == 128 ? 2 : 1;             // key tiles, and value tiles, in shared memory
+    static constexpr int Q_TILE = 128 * D * 2, K_TILE = kKeys * D * 2, V_TILE = K_TILE;
+    static constexpr int SOFT_WARPS = 4 * NT, UNPACK_WARPS = 8;
+    static constexpr int MMA_WARP = SOFT_WARPS + UNPACK_WARPS, THREADS = 32 * (MMA_WARP + 4);
+    // registers: of the launch, and of the softmax, unpacking and product warps afterwards (the sums agree)
+    static constexpr int REGS = D == 128 ? 96 : 128;
+    static constexpr int SOFT_REGS = D == 128 ? 104 : 128, UNPACK_REGS = D == 128 ? 104 : 152, MMA_REGS = D == 128 ? 64 : 80;
+    static_assert(SOFT_WARPS * SOFT_REGS + UNPACK_WARPS * UNPACK_REGS + 4 * MMA_REGS <= (MMA_WARP + 4) * REGS, "register split");
+    static constexpr int OFF_Q = 0, OFF_K = OFF_Q + NT * Q_TILE, OFF_V = OFF_K + STAGES * K_TILE;
+    static constexpr int OFF_FAC = OFF_V + STAGES * V_TILE;     // factor of every row's scores
+    static constexpr int OFF_NAN = OFF_FAC + ROWS * 4;          // 64-bit word per channel, see note_nan
+    static constexpr int OFF_BAR = OFF_NAN + D * 8;
+    static constexpr int OFF_MISC = OFF_BAR + 256;
+    static constexpr int OFF_WALK = OFF_MISC + 128;             // a Walk per warp
+    static constexpr int SMEM = OFF_WALK + 32 * (int)sizeof(Walk) + 1024;           // the tiles start on a 1,024-byte boundary
+    static_assert(SMEM <= 232448, "shared memory of a block");
 };
 
 // ---- plan -------------------------------------------------------------------------------------------
@@ -356,11 +365,23 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&r)[32])
                    "f"(r[18]), "f"(r[19]), "f"(r[20]), "f"(r[21]), "f"(r[22]), "f"(r[23]), "f"(r[24]), "f"(r[25]), "f"(r[26]),
                    "f"(r[27]), "f"(r[28]), "f"(r[29]), "f"(r[30]), "f"(r[31]) : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
+__device__ __forceinline__ void tmem_ld8_u32(uint32_t taddr, uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_n(uint32_t taddr, float (&r)[32]) { tmem_ld32(taddr, r); }
+__device__ __forceinline__ void tmem_st_n(uint32_t taddr, const uint32_t (&r)[16])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
                  ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
                    "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_st_n(uint32_t taddr, const uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 // two fp32 operations in one instruction
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
@@ -427,32 +448,19 @@ __device__ __forceinline__ int stale_row(int e, int t)
 }
 // So key row n is token 2 (n / 16 mod 4) + 8 (n / 2 mod 2) + n mod 2 of run 4 (n / 64) + 2 (n / 8 mod 2) + n / 4 mod 2.
 
-// Entry of a run of 16 tokens in a list, looked up one key tile (eight runs) ahead of its use.
+// A run of 16 tokens in a list of pages; moves on by a key tile (eight runs).
 struct Cursor {
-    const int2* list;
-    int page, sub, run, n, tiles, step;       // step: 1, or -1 for the list that grows from the back
-    int2 entry;                               // logical page, id; valid where ok
-    bool ok;
+    int page, sub, left;                      // page of the list, run within it, runs from here to the end of the list
 
-    __device__ __forceinline__ void open(const int2* l, int r, int count, int t, int direction)
+    __device__ __forceinline__ void open(int run, int n, int tiles)
     {
-        list = l; run = r; n = count; tiles = t; step = direction;
-        page = r / t;
-        sub = r - page * t;
-        look();
+        page = run / tiles;
+        sub = run - page * tiles;
+        left = n - run;
     }
-    __device__ __forceinline__ void look()
+    __device__ __forceinline__ void next(int tiles)
     {
-        ok = run < n;
-        entry = make_int2(0, 0);
-        if (ok) {
-            const uint2 v = ldg64(list + (long long)step * page);
-            entry = make_int2((int)v.x, (int)v.y);
-        }
-    }
-    __device__ __forceinline__ void next()
-    {
-        run += 8;
+        left -= 8;
         if (tiles == 1) page += 8;
         else {
             sub += 8;
@@ -462,7 +470,6 @@ struct Cursor {
                 sub -= q * tiles;
             }
         }
-        look();
     }
 };
 
@@ -472,7 +479,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
 {
     using G = Geo<D>;
     using namespace tm;
-    constexpr int NT = G::NT, ROWS = G::ROWS;
+    constexpr int NT = G::NT, ROWS = G::ROWS, COLS = G::COLS;
     constexpr uint32_t FULL = 0xffffffffu;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_at = smem_u32(smem_raw), sb = (raw_at + 1023) & ~1023u;
@@ -545,8 +552,16 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
     tc_fence_after();
     const uint32_t tb = *tmem_s;
     constexpr uint32_t kColS = NT * D;                           // O: NT x D columns, then two score buffers
-    Walker<ROWS> walk(P, share);
-    Segment s;
+    Walk* walk = reinterpret_cast<Walk*>(smem + G::OFF_WALK) + warp;
+    const Segment& s = walk->s;
+    if (lane == 0) walk->open(P, share);
+    __syncwarp();
+    auto next_segment = [&]() -> bool {
+        __syncwarp();                                            // the segment before is no longer looked at
+        bool more = false;
+        if (lane == 0) more = walk->next<ROWS>(P, share);
+        return __any_sync(FULL, more);
+    };
 
     // Bounded by wall time: a wait that gives up flags the pool and lets every later wait of the block pass.  Polls are few
     // instructions, since they take issue slots from the working warps.
@@ -573,7 +588,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
         if (warp == G::MMA_WARP) {
             constexpr uint32_t kTb = 0;                          // the whole of tensor memory is this block's
             uint32_t job = 0, tile = 0, fills = 0;               // scores, key tiles and queries so far
-            while (uniform(walk.next(P, share, s))) {
+            while (next_segment()) {
                 const int nt = (int)uniform(s.nt), n = (int)uniform(s.t1 - s.t0) * nt;
                 const int turn = (int)uniform(max(s.u.stale_tiles - s.t0, 0));        // key tile of the segment that starts the FP8 ones
                 // job i of the segment: key tile t0 + i / nt, row tile i % nt; its scores are issued two jobs ahead
@@ -640,12 +655,13 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(i));
         };
-        while (walk.next(P, share, s)) {
+        while (next_segment()) {
             ++segments;
             const int first_pos = s.r.len - s.r.n_new + s.rt * ROWS / P.group;        // of the unit's first row
             const int rows = min(ROWS, s.r.n_new * P.group - s.rt * ROWS);
             const int2* list = P.list + (size_t)s.b * P.max_pages;
             const size_t page8 = fp8_page_bytes(D, P.tiles), page3 = tq3_page_bytes(D, P.tiles);
+            const uint32_t stride8 = (uint32_t)(P.hkv * page8), stride3 = (uint32_t)(P.hkv * page3);     // of a page (launch checks)
             const uint8_t* base8 = P.fp8 + s.h * page8;
             const uint8_t* base3 = P.tq3 + s.h * page3;
 
@@ -772,84 +788,90 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                 }
             };
 
-            const int cut = s.u.stale_tiles;
+            const int cut = s.u.stale_tiles, len = s.r.len;
             if (s.t0 < cut) {
-                // ---- Stale tiles: keys of run w; values of the two runs w & ~1, w | 1, half of the channels
-                constexpr int LW = 3 * D / 64;                   // packed words of a lane per section
+                // ---- Stale tiles.  Keys: a warp per run.  Values: two warps for two runs (whose shares make up 16-byte
+                // chunks), half of the channels each.
+                constexpr int KW = 3 * D / 64, BLOCKS = D / 32;  // packed key words of a lane, 16-channel blocks of a warp
                 const int n_tiles = min(s.t1, cut), half = w & 1;
-                Cursor kc, vc[2];
-                kc.open(list, s.t0 * 8 + w, s.r.n_stale, P.tiles, 1);
-#pragma unroll
-                for (int e = 0; e < 2; ++e) vc[e].open(list, s.t0 * 8 + (w & ~1) + e, s.r.n_stale, P.tiles, 1);
-                uint32_t kw[LW], gw, vw[2][LW / 2 + (LW / 2 & 1)], mw[2][D / 32][2];
+                // Ids of the runs to load next, looked up a tile ahead.  Nothing here may look at what a load brings: that
+                // would hold the warp until it is there.  So runs behind the list's end load its last page, and are cleared
+                // where they are unpacked.
+                const int last_page = (s.r.n_stale + P.tiles - 1) / P.tiles - 1;
+                Cursor kc, vc;
+                int k_id, v_id[2], k_live, v_live;               // live: runs that the loaded words hold
+                kc.open(s.t0 * 8 + w, s.r.n_stale, P.tiles);
+                vc.open(s.t0 * 8 + (w & ~1), s.r.n_stale, P.tiles);
+                auto look_keys = [&] { k_id = (int)ldg32(&list[min(kc.page, last_page)].y); };
+                auto look_values = [&] {                         // a run and the one behind it
+                    v_id[0] = (int)ldg32(&list[min(vc.page, last_page)].y);
+                    v_id[1] = (int)ldg32(&list[min(vc.page + (vc.sub + 1 == P.tiles ? 1 : 0), last_page)].y);
+                };
+                look_keys();
+                look_values();
+                uint32_t kw[KW], gw[2], vw[2][KW / 2 + (KW / 2 & 1)], mw[2][BLOCKS][2];
                 auto load_keys = [&] {                           // of the tile that kc is at, which moves on
-                    if (!kc.ok) {
+                    const uint8_t* r = base3 + (unsigned long long)(uint32_t)k_id * stride3 + kc.sub * (uint32_t)(12 * D + 32);
 #pragma unroll
-                        for (int i = 0; i < LW; ++i) kw[i] = 0;
-                        gw = 0;
-                        return;
-                    }
-                    const uint8_t* r = base3 + (size_t)kc.entry.y * P.hkv * page3 + (size_t)kc.sub * tq3_tile_bytes(D);
-#pragma unroll
-                    for (int c = 0; c < LW / 4; ++c) {
+                    for (int c = 0; c < KW / 4; ++c) {
                         const uint4 v = ldg128(r + c * 512 + lane * 16);
                         kw[4 * c] = v.x; kw[4 * c + 1] = v.y; kw[4 * c + 2] = v.z; kw[4 * c + 3] = v.w;
                     }
-                    if constexpr (LW % 4 != 0) {
-                        const uint2 v = ldg64(r + (LW / 4) * 512 + lane * 8);
-                        kw[LW - 2] = v.x; kw[LW - 1] = v.y;
+                    if constexpr (KW % 4 != 0) {
+                        const uint2 v = ldg64(r + (KW / 4) * 512 + lane * 8);
+                        kw[KW - 2] = v.x; kw[KW - 1] = v.y;
                     }
-                    gw = ldg16(r + 12 * D + 2 * g) | ldg16(r + 12 * D + 2 * g + 16) << 16;      // g of tokens g and g + 8
-                    kc.next();
+                    gw[0] = ldg16(r + 12 * D + 2 * g);           // g of tokens g and g + 8
+                    gw[1] = ldg16(r + 12 * D + 2 * g + 16);
+                    k_live = kc.left;
+                    kc.next(P.tiles);
+                    look_keys();
                 };
                 auto load_values = [&] {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        if (!vc[e].ok) {
-#pragma unroll
-                            for (int i = 0; i < (int)(sizeof vw[0] / 4); ++i) vw[e][i] = 0;
-#pragma unroll
-                            for (int i = 0; i < D / 32; ++i) mw[e][i][0] = mw[e][i][1] = 0;
-                            continue;
-                        }
-                        const uint8_t* page = base3 + (size_t)vc[e].entry.y * P.hkv * page3;
-                        const uint8_t* v = page + (size_t)vc[e].sub * tq3_tile_bytes(D) + 6 * D;
-                        const uint8_t* meta = page + (size_t)P.tiles * tq3_tile_bytes(D);
+                        const uint8_t* page = base3 + (unsigned long long)(uint32_t)v_id[e] * stride3;
+                        const int sub = e == 0 ? vc.sub : vc.sub + 1 == P.tiles ? 0 : vc.sub + 1;
+                        const uint8_t* at = page + sub * (uint32_t)(12 * D + 32) + 6 * D + lane * 16;
                         if constexpr (D == 256) {                // words 0-5 or 6-11 of the lane
                             if (half == 0) {
-                                const uint4 a = ldg128(v + lane * 16);
-                                const uint2 c = ldg64(v + 512 + lane * 16);
+                                const uint4 a = ldg128(at);
+                                const uint2 c = ldg64(at + 512);
                                 vw[e][0] = a.x; vw[e][1] = a.y; vw[e][2] = a.z; vw[e][3] = a.w; vw[e][4] = c.x; vw[e][5] = c.y;
                             } else {
-                                const uint2 a = ldg64(v + 512 + lane * 16 + 8);
-                                const uint4 c = ldg128(v + 1024 + lane * 16);
+                                const uint2 a = ldg64(at + 512 + 8);
+                                const uint4 c = ldg128(at + 1024);
                                 vw[e][0] = a.x; vw[e][1] = a.y; vw[e][2] = c.x; vw[e][3] = c.y; vw[e][4] = c.z; vw[e][5] = c.w;
                             }
                         } else {                                 // words 0-2 or 3-5
                             if (half == 0) {
-                                const uint4 a = ldg128(v + lane * 16);
+                                const uint4 a = ldg128(at);
                                 vw[e][0] = a.x; vw[e][1] = a.y; vw[e][2] = a.z;
                             } else {
-                                const uint32_t a = ldg32(v + lane * 16 + 12);
-                                const uint2 c = ldg64(v + 512 + lane * 8);
-                                vw[e][0] = a; vw[e][1] = c.x; vw[e][2] = c.y;
+                                vw[e][0] = ldg32(at + 12);
+                                const uint2 c = ldg64(at + 512 - lane * 8);
+                                vw[e][1] = c.x; vw[e][2] = c.y;
                             }
                         }
-                        // scale / zero of the block pairs of these channels: (sc g, sc g+8), (zp g, zp g+8), twice
+                        // scale / zero of the warp's block pairs: (sc g, sc g+8), (zp g, zp g+8), twice
+                        const uint8_t* meta = page + P.tiles * (uint32_t)(12 * D + 32) + half * (D / 64) * 128 + g * 16;
 #pragma unroll
-                        for (int i = 0; i < D / 64; ++i) {
-                            const uint4 m = ldg128(meta + (half * (D / 64) + i) * 128 + g * 16);
+                        for (int i = 0; i < BLOCKS / 2; ++i) {
+                            const uint4 m = ldg128(meta + i * 128);
                             mw[e][2 * i][0] = m.x; mw[e][2 * i][1] = m.y; mw[e][2 * i + 1][0] = m.z; mw[e][2 * i + 1][1] = m.w;
                         }
-                        vc[e].next();
                     }
+                    v_live = vc.left;
+                    vc.next(P.tiles);
+                    look_values();
                 };
                 auto put_keys = [&] {
                     const uint32_t st = k_tile % G::STAGES;
                     if (k_tile >= G::STAGES) wait(kKEmpty + st, (k_tile / G::STAGES & 1) ^ 1);
                     const uint32_t k_at = sb + G::OFF_K + st * G::K_TILE;
                     const int n0 = stale_row(w, g), n1 = stale_row(w, g + 8);
-                    const uint32_t g0 = hmul2_u32(prmt(gw, gw, 0x1010u), k_unit), g1 = hmul2_u32(prmt(gw, gw, 0x3232u), k_unit);
+                    const uint32_t g0 = k_live > 0 ? hmul2_u32(prmt(gw[0], gw[0], 0x1010u), k_unit) : 0u;        // no run: zeros
+                    const uint32_t g1 = k_live > 0 ? hmul2_u32(prmt(gw[1], gw[1], 0x1010u), k_unit) : 0u;
 #pragma unroll
                     for (int j = 0; j < D / 64; ++j) {
                         const uint32_t A = kw[3 * j], Bw = kw[3 * j + 1], Cw = kw[3 * j + 2];
@@ -881,48 +903,55 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                     ++k_tile;
                 };
                 auto put_values = [&] {
+                    if (v_live < 2) {                            // no second run, or none: scale and zero of 0
+#pragma unroll
+                        for (int i = 0; i < BLOCKS; ++i) {
+                            mw[1][i][0] = mw[1][i][1] = 0;
+                            if (v_live < 1) mw[0][i][0] = mw[0][i][1] = 0;
+                        }
+                    }
                     if (P.ve != 0) {
 #pragma unroll
                         for (int e = 0; e < 2; ++e)
 #pragma unroll
-                            for (int i = 0; i < D / 32; ++i) {
+                            for (int i = 0; i < BLOCKS; ++i) {
                                 mw[e][i][0] = hmul2_u32(mw[e][i][0], v_unit);
                                 mw[e][i][1] = hmul2_u32(mw[e][i][1], v_unit);
                             }
                     }
                     const uint32_t st = v_tile % G::STAGES;
                     if (v_tile >= G::STAGES) wait(kVEmpty + st, (v_tile / G::STAGES & 1) ^ 1);
-                    const uint32_t v_at = sb + G::OFF_V + st * G::V_TILE + (w >> 2) * (D * 128);
-                    const int c = 2 * tq + ((w >> 1) & 1);
+                    const int c = 2 * tq + ((w >> 1) & 1), ch0 = half * (D / 2) + g;
+                    const uint32_t v_at = sb + G::OFF_V + st * G::V_TILE + (w >> 2) * (D * 128) + chunk_at(ch0, c);
 #pragma unroll
                     for (int j = 0; j < D / 128; ++j) {          // 64 channels: four blocks of 16
-                        uint32_t X0[2], X1[2];
+                        uint32_t X[2][2];
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            X0[e] = prmt(vw[e][3 * j], vw[e][3 * j + 1], 0x6341u);
-                            X1[e] = prmt(vw[e][3 * j + 1], vw[e][3 * j + 2], 0x6341u);
+                            X[e][0] = prmt(vw[e][3 * j], vw[e][3 * j + 1], 0x6341u);
+                            X[e][1] = prmt(vw[e][3 * j + 1], vw[e][3 * j + 2], 0x6341u);
                         }
-#pragma unroll
-                        for (int blk = 0; blk < 4; ++blk) {
+                        auto put_block = [&](auto block) {       // rows g and g + 8
+                            constexpr int B4 = decltype(block)::value;
+                            const int i = 4 * j + B4;
                             uint32_t o[2][4];                    // run e: row g (tokens low, high), row g + 8 (low, high)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                const uint32_t W0 = vw[e][3 * j], W1 = vw[e][3 * j + 1], W2 = vw[e][3 * j + 2];
                                 uint32_t a[4];
-                                if (blk == 0) value_operands<0>(a, W0, W1, W2, X0[e]);
-                                else if (blk == 1) value_operands<1>(a, W0, W1, W2, X0[e]);
-                                else if (blk == 2) value_operands<2>(a, W0, W1, W2, X1[e]);
-                                else value_operands<3>(a, W0, W1, W2, X1[e]);
-                                const __half2 sc = as_half2(mw[e][4 * j + blk][0]), zp = as_half2(mw[e][4 * j + blk][1]);
+                                value_operands<B4>(a, vw[e][3 * j], vw[e][3 * j + 1], vw[e][3 * j + 2], X[e][B4 >> 1]);
+                                const __half2 sc = as_half2(mw[e][i][0]), zp = as_half2(mw[e][i][1]);
                                 o[e][0] = as_u32(__hfma2(as_half2(a[0]), __low2half2(sc), __low2half2(zp)));
                                 o[e][1] = as_u32(__hfma2(as_half2(a[2]), __low2half2(sc), __low2half2(zp)));
                                 o[e][2] = as_u32(__hfma2(as_half2(a[1]), __high2half2(sc), __high2half2(zp)));
                                 o[e][3] = as_u32(__hfma2(as_half2(a[3]), __high2half2(sc), __high2half2(zp)));
                             }
-                            const int ch = half * (D / 2) + 64 * j + 16 * blk + g;
-                            sts128(v_at + chunk_at(ch, c), o[0][0], o[0][1], o[1][0], o[1][1]);
-                            sts128(v_at + chunk_at(ch + 8, c), o[0][2], o[0][3], o[1][2], o[1][3]);
-                        }
+                            sts128(v_at + i * 2048, o[0][0], o[0][1], o[1][0], o[1][1]);
+                            sts128(v_at + i * 2048 + 1024, o[0][2], o[0][3], o[1][2], o[1][3]);
+                        };
+                        put_block(Int<0>{});
+                        put_block(Int<1>{});
+                        put_block(Int<2>{});
+                        put_block(Int<3>{});
                     }
                     arrive(kVFull + st);
                     ++v_tile;
@@ -932,8 +961,8 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                 fill_query(true);
                 put_keys();
                 load_keys();
-                for (int t = s.t0; t < n_tiles; ++t) {
-                    if (t + 1 < n_tiles) {
+                for (int t = n_tiles - s.t0; t > 0; --t) {
+                    if (t > 1) {
                         put_keys();
                         load_keys();
                     }
@@ -945,27 +974,40 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                 // ---- FP8 tiles: a warp per run
                 constexpr int N = 16 * D / 512;                  // 16-byte loads of a lane for a run's keys, or values
                 const int t_first = max(s.t0, cut);
-                Cursor kc, vc;
-                kc.open(list + P.max_pages - 1, (t_first - cut) * 8 + w, s.u.n_fp8, P.tiles, -1);
-                vc = kc;
+                // the run to load next (keys), looked up a tile ahead as above, and that of the tile before it (values)
+                const int last_page = (s.u.n_fp8 + P.tiles - 1) / P.tiles - 1;
+                Cursor kc;
+                uint2 k_page, v_page;
+                int k_sub, v_sub, k_left, v_left;
+                kc.open((t_first - cut) * 8 + w, s.u.n_fp8, P.tiles);
+                auto look = [&] {
+                    k_page = ldg64(&list[P.max_pages - 1 - min(kc.page, last_page)]);
+                    k_sub = kc.left > 0 ? kc.sub : 0;
+                    k_left = kc.left;
+                };
+                look();
                 uint4 kr[N], vr[N];
-                int v_pos = 0, left = 0;                         // of the run whose values are loaded: first position, tokens that exist
-                auto load = [&](uint4 (&x)[N], Cursor& c, int off) {
-                    const uint8_t* rec = base8 + (size_t)c.entry.y * P.hkv * page8 + (size_t)c.sub * fp8_record_bytes(D) + off;
+                int v_lp, v_at_sub, v_live;                      // of the run whose values are loaded
+                auto load = [&](uint4 (&x)[N], uint32_t id, int sub, int off) {
+                    const uint8_t* rec = base8 + (unsigned long long)id * stride8 + sub * (uint32_t)(32 * D) + off;
 #pragma unroll
-                    for (int i = 0; i < N; ++i) x[i] = c.ok ? ldg128(rec + i * 512) : make_uint4(0, 0, 0, 0);
+                    for (int i = 0; i < N; ++i) x[i] = ldg128(rec + i * 512);
                 };
                 // eight lanes take 64 dims of two keys: their 16-byte stores meet every bank once
                 const int k_tok = (D == 128 ? 2 * (lane >> 4) : 0) + ((lane >> 2) & 1), k_atom = D == 128 ? (lane >> 3) & 1 : lane >> 3;
-                auto load_keys = [&] {
-                    load(kr, kc, k_tok * D + k_atom * 64 + (lane & 3) * 16);
-                    kc.next();
-                };
+                auto load_keys = [&] { load(kr, k_page.y, k_sub, k_tok * D + k_atom * 64 + (lane & 3) * 16); };
                 auto load_values = [&] {
-                    load(vr, vc, 16 * D + lane * 16);
-                    v_pos = (vc.entry.x * P.tiles + vc.sub) * kPage;
-                    left = vc.ok ? s.r.len - v_pos : 0;
-                    vc.next();
+                    load(vr, v_page.y, v_sub, 16 * D + lane * 16);
+                    v_lp = (int)v_page.x;
+                    v_at_sub = v_sub;
+                    v_live = v_left;
+                };
+                auto move_on = [&] {
+                    v_page = k_page;
+                    v_sub = k_sub;
+                    v_left = k_left;
+                    kc.next(P.tiles);
+                    look();
                 };
                 auto put_keys = [&] {
                     const uint32_t st = k_tile % G::STAGES;
@@ -991,6 +1033,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                 auto put_values = [&] {
                     const uint32_t st = v_tile % G::STAGES;
                     if (v_tile >= G::STAGES) wait(kVEmpty + st, (v_tile / G::STAGES & 1) ^ 1);
+                    const int v_pos = (v_lp * P.tiles + v_at_sub) * kPage, left = v_live > 0 ? len - v_pos : 0;   // tokens that exist
                     if (left < kPage) {                          // what no token fills may be anything
 #pragma unroll
                         for (int i = 0; i < N; ++i) {
@@ -1031,12 +1074,14 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                     ++v_tile;
                 };
                 load_keys();
+                move_on();
                 load_values();
                 fill_query(false);
                 put_keys();
                 load_keys();
-                for (int t = t_first; t < s.t1; ++t) {
-                    if (t + 1 < s.t1) {
+                for (int t = s.t1 - t_first; t > 0; --t) {
+                    move_on();
+                    if (t > 1) {
                         put_keys();
                         load_keys();
                     }
@@ -1047,7 +1092,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
         }
     } else {
         // ================= softmax and output =================
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(G::SOFT_REGS));
+        if constexpr (G::SOFT_REGS > G::REGS) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(G::SOFT_REGS));
         const int t = warp >> 2;                                 // row tile
         const uint32_t my_lanes = (uint32_t)(32 * (warp & 3)) << 16;
         const int my_row = t * 128 + (warp & 3) * 32 + lane;     // within the unit
@@ -1057,7 +1102,22 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(i));
         };
-        while (walk.next(P, share, s)) {
+        while (next_segment()) {
+            // the output so far times f (a factor of the row), once the products issued so far are done.  (The product before
+            // the last is: the scores looked at were issued behind it.  So the barrier's parity is the last one's.)
+            auto scale_output = [&](float f) {
+                wait(kPvDone + t, (done - 1) & 1);
+                tc_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < D / 8; ++c) {
+                    uint32_t y[8];
+                    tmem_ld8_u32(col_o + 8 * c, y);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * f);
+                    tmem_st_n(col_o + 8 * c, y);
+                }
+            };
             ++segments;
             const int row = s.rt * ROWS + my_row, n_rows = s.r.n_new * P.group;
             const bool live = row < n_rows, warp_live = row - lane < n_rows;
@@ -1069,25 +1129,26 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
             const bool ordinary = s.r.exact && s.r.stale_end * kPage <= first_pos + 1;     // every Stale page lies before the first row
             float ref = -CUDART_INF_F, sum = 0.f, fac = 0.f;
             int n_done = 0;                                      // key tiles of this segment so far
-            for (int kt = s.t0; kt < s.t1; ++kt) {
+            const int t0 = s.t0, t1 = s.t1, nt = s.nt, n_stale = s.r.n_stale, n_fp8 = s.u.n_fp8, all_fp8 = s.r.n_fp8;
+            for (int kt = t0; kt < t1; ++kt) {
                 const bool stale = kt < cut;
                 bool turn = false;                               // from Stale values' unit to the FP8 values'
-                if (kt == s.t0 || kt == cut) {
+                if (kt == t0 || kt == cut) {
                     wait(kQFull, fills++ & 1);
                     fac = fac_s[my_row];
                     warp_arrive(kFacRead);
-                    turn = kt > s.t0 && P.v_scale != __uint_as_float((uint32_t)(127 + P.ve) << 23);
+                    turn = kt > t0 && P.v_scale != __uint_as_float((uint32_t)(127 + P.ve) << 23);
                 }
-                if (t >= s.nt) continue;
-                const uint32_t i = job + (uint32_t)(kt - s.t0) * s.nt + t, buf = i & 1;
+                if (t >= nt) continue;
+                const uint32_t i = job + (uint32_t)(kt - t0) * nt + t, buf = i & 1;
                 wait(kSFull + buf, (i >> 1) & 1);
                 tc_fence_after();
                 const uint32_t col_s = tb + my_lanes + kColS + kKeys * buf;
                 if (warp_live) {
                     // masks are looked at where the tile is not full, or its last run passes the first row's position
-                    const int n_in = min(8, (stale ? s.r.n_stale : s.u.n_fp8) - (stale ? kt : kt - cut) * 8);
+                    const int n_in = min(8, (stale ? n_stale : n_fp8) - (stale ? kt : kt - cut) * 8);
                     bool masked = n_in < 8 || !ordinary;
-                    if (!masked && !stale) masked = (runs - s.r.n_fp8 + (kt - cut) * 8 + 7) * kPage + kPage - 1 > first_pos;
+                    if (!masked && !stale) masked = (runs - all_fp8 + (kt - cut) * 8 + 7) * kPage + kPage - 1 > first_pos;
                     if (masked) {                                // what the row does not see becomes -inf in tensor memory
 #pragma unroll 1
                         for (int c = 0; c < 4; ++c) {
@@ -1116,52 +1177,50 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                         }
                         tmem_wait_st();
                     }
-                    float mx;
-                    {
-                        float m4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+                    const float2 fac2 = make_float2(fac, fac);
+                    if (turn) scale_output(__uint_as_float((uint32_t)(127 + P.ve) << 23) / P.v_scale);
+                    // Exponentials against the reference so far; where a score exceeds it by too much (as a rule only in a
+                    // unit's first tile) it is raised by whole powers of two, and what was summed or stored before is scaled
+                    // down exactly
 #pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {
-                            float x[32];
-                            tmem_ld32(col_s + 32 * c, x);
-                            tmem_wait_ld();
+                    for (int c = 0; c < kKeys / COLS; ++c) {
+                        float x[COLS], m4[4];
+                        tmem_ld_n(col_s + COLS * c, x);
+                        tmem_wait_ld();
 #pragma unroll
-                            for (int k = 0; k < 32; k += 2) m4[(k >> 1) & 3] = fmaxf(m4[(k >> 1) & 3], fmaxf(x[k], x[k + 1]));
-                        }
-                        mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * fac;
-                    }
-                    const bool raise = mx > ref + (kShift + kSlack);
-                    if (__any_sync(FULL, raise) || turn) {
-                        const float to = raise ? mx - kShift : ref;
-                        const float f = raise ? (ref == -CUDART_INF_F ? 0.f : fast_exp2(ref - to)) : 1.f;
-                        ref = to;
-                        sum *= f;
-                        if (n_done > 0) {
-                            const float fo = turn ? f * (__uint_as_float((uint32_t)(127 + P.ve) << 23) / P.v_scale) : f;
-                            // the product before that one is done (these scores were issued behind it), so the parity is this one's
-                            wait(kPvDone + t, (done - 1) & 1);
-                            tc_fence_after();
-                            float x[32];
+                        for (int q = 0; q < 4; ++q) m4[q] = fmaxf(x[q], x[q + 4]);
+#pragma unroll
+                        for (int k = 8; k < COLS; k += 8)
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) m4[q] = fmaxf(m4[q], fmaxf(x[k + q], x[k + q + 4]));
+                        const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * fac;
+                        const bool raise = mx > ref + (kShift + kSlack);
+                        if (__any_sync(FULL, raise)) {
+                            float f = 1.f;
+                            if (raise) {
+                                const float to = ref == -CUDART_INF_F ? mx - kShift : ref + ceilf(mx - kShift - ref);
+                                f = ref == -CUDART_INF_F ? 0.f : exp2f(ref - to);
+                                ref = to;
+                            }
+                            sum *= f;
+                            if (n_done > 0) scale_output(f);
+                            const uint32_t f2 = pack_f16x2(f, f);
 #pragma unroll 1
-                            for (int c = 0; c < D / 32; ++c) {
-                                tmem_ld32(col_o + 32 * c, x);
+                            for (int p = 0; p < c * COLS / 16; ++p) {    // the probabilities of the columns before these
+                                uint32_t y[8];
+                                tmem_ld8_u32(col_s + 8 * p, y);
                                 tmem_wait_ld();
 #pragma unroll
-                                for (int k = 0; k < 32; ++k) x[k] *= fo;
-                                tmem_st32(col_o + 32 * c, x);
+                                for (int k = 0; k < 8; ++k) y[k] = hmul2_u32(y[k], f2);
+                                tmem_st_n(col_s + 8 * p, y);
                             }
                         }
-                    }
-                    const float base = ref == -CUDART_INF_F ? 0.f : ref;
-                    const float2 fac2 = make_float2(fac, fac), base2 = make_float2(-base, -base);
-#pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        float x[32];
-                        uint32_t h2[16];
-                        tmem_ld32(col_s + 32 * c, x);
-                        tmem_wait_ld();
+                        const float base = ref == -CUDART_INF_F ? 0.f : ref;
+                        const float2 base2 = make_float2(-base, -base);
                         float2 s2 = make_float2(0.f, 0.f);
+                        uint32_t h2[COLS / 2];
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) {
+                        for (int k = 0; k < COLS / 2; ++k) {
                             float2 e = fma2(make_float2(x[2 * k], x[2 * k + 1]), fac2, base2);
                             e.x = fast_exp2(e.x);
                             e.y = fast_exp2(e.y);
@@ -1169,7 +1228,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                             h2[k] = pack_f16x2(e.x, e.y);
                         }
                         sum += s2.x + s2.y;
-                        tmem_st16(col_s + 16 * c, h2);
+                        tmem_st_n(col_s + COLS / 2 * c, h2);
                     }
                     tmem_wait_st();
                 }
@@ -1323,6 +1382,10 @@ static int32_t launch(const Params& P, int sms, cudaStream_t s)
         return MKV_E_CUDA;
     }
     MKV_CUDA(cudaFuncSetAttribute(chunk_scan_kernel<D, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM));
+    if ((unsigned long long)P.hkv * fp8_page_bytes(D, P.tiles) >> 32) {
+        set_last_error("chunk attention: a page of all KV heads has 4 GB or more");
+        return MKV_E_INVALID;
+    }
     const int blocks = sms < kMaxBlocks ? sms : kMaxBlocks;
     MKV_CUDA(launch_pdl(chunk_plan_kernel<G::ROWS>, dim3(P.B), kPlanThreads, 0, 1, s, P));
     MKV_CUDA(launch_pdl(chunk_scan_kernel<D, FMT>, dim3(blocks), G::THREADS, G::SMEM, 1, s, P));
