@@ -35,8 +35,8 @@ namespace chunk {
 
 constexpr int kMaxBlocks = 160;              // of the scan's grid: sizes the partials
 constexpr int kKeys = 128;                   // keys of a tile: eight runs of 16 tokens
-constexpr int kUnitCost = 2;                 // what a unit costs besides its key tiles (query, epilogue), in key tiles
-constexpr int kLeastShare = 3;               // key tiles of a block at least
+constexpr int kUnitCost = 6;                 // what a unit costs besides its key tiles (query, epilogue), in key tiles
+constexpr int kLeastShare = 2;               // key tiles of a block at least
 constexpr float kShift = 7.f, kSlack = 8.f;  // see above: probabilities are at most 2^(kShift + kSlack)
 constexpr int kNoPos = 0x7fffffff;
 
@@ -87,9 +87,10 @@ enum {
     kKFull = 0, kKEmpty = 2, kVFull = 4, kVEmpty = 6,           // [stage]
     kSFull = 8, kPFull = 10,                                    // [score buffer]
     kPvDone = 12,                                               // [row tile]
-    kQFull = 14, kFacRead = 15, kSegDone = 16, kDrained = 17,
-    kOutput = 18,                                               // [row tile] the last product of a segment
-    kBars = 20
+    kQFull = 14, kFacRead = 15, kDrained = 16,
+    kOutput = 17,                                               // [row tile] the last product of a segment
+    kJoin = 19, kJoined = 23,                                   // [warp of a softmax group] rows handed over, and taken
+    kBars = 27
 };
 
 // ---- the units --------------------------------------------------------------------------------------
@@ -197,7 +198,8 @@ struct Geo {
     static constexpr int OFF_Q = 0, OFF_K = OFF_Q + NT * Q_TILE, OFF_V = OFF_K + STAGES * K_TILE;
     static constexpr int OFF_FAC = OFF_V + STAGES * V_TILE;     // factor of every row's scores
     static constexpr int OFF_NAN = OFF_FAC + ROWS * 4;          // 64-bit word per channel, see note_nan
-    static constexpr int OFF_BAR = OFF_NAN + D * 8;
+    static constexpr int OFF_PAIR = OFF_NAN + D * 8;            // 16 bytes a row: what the second of two softmax groups hands over
+    static constexpr int OFF_BAR = OFF_PAIR + (NT == 2 ? 128 * 16 : 0);
     static constexpr int OFF_MISC = OFF_BAR + 256;
     static constexpr int OFF_WALK = OFF_MISC + 128;             // a Walk per warp
     static constexpr int SMEM = OFF_WALK + 32 * (int)sizeof(Walk) + 1024;           // the tiles start on a 1,024-byte boundary
@@ -213,12 +215,12 @@ template <int ROWS>
 __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const Params P)
 {
     __shared__ int warp_sum[2][kPlanThreads / 32];
-    __shared__ int bad_s, stale_end_s;
+    __shared__ int bad_s, stale_end_s, open_s;                  // open: the last page is an FP8 one
     __shared__ long long cost_s;
     pdl_begin();
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int T = P.tiles * kPage;
-    if (tid == 0) { bad_s = 0; stale_end_s = 0; cost_s = 0; }
+    if (tid == 0) { bad_s = 0; stale_end_s = 0; open_s = 0; cost_s = 0; }
     int len = P.lens[b];
     const int first = P.starts[b], last = P.starts[b + 1];
     uint32_t flags = 0;
@@ -270,6 +272,7 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const Params P
             if (stale >> i & 1) list[at3++] = make_int2(p0 + i, id[i]);
             else if (fp8 >> i & 1) list[P.max_pages - 1 - at8++] = make_int2(p0 + i, id[i]);
         }
+        if (pages - 1 - p0 >= 0 && pages - 1 - p0 < kPlanPer && (fp8 >> (pages - 1 - p0) & 1)) open_s = 1;
         if (stale) atomicMax(&stale_end_s, (p0 + 32 - __clz(stale)) * P.tiles);
         __syncthreads();
     }
@@ -284,7 +287,7 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const Params P
     r.n_fp8 = n_fp8 * P.tiles;
     // an open last page counts its filled runs (an open page is FP8, or it is in no list)
     r.exact = !bad_s;
-    if (pages > 0 && n_fp8 > 0 && list[P.max_pages - n_fp8].x == pages - 1)
+    if (open_s)
         r.n_fp8 -= P.tiles - ((len - (pages - 1) * T + kPage - 1) / kPage);
     r.stale_end = stale_end_s;
     const int n_rt = (n_new * P.group + ROWS - 1) / ROWS;
@@ -372,6 +375,13 @@ __device__ __forceinline__ void tmem_ld8_u32(uint32_t taddr, uint32_t (&r)[8])
                  : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_ld_n(uint32_t taddr, float (&r)[32]) { tmem_ld32(taddr, r); }
+__device__ __forceinline__ void tmem_ld_n(uint32_t taddr, float (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]),
+                   "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
+                 : "r"(taddr) : "memory");
+}
 __device__ __forceinline__ void tmem_st_n(uint32_t taddr, const uint32_t (&r)[16])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
@@ -396,6 +406,13 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
     float2 r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<unsigned long long&>(r))
         : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+    return r;
+}
+// fast_exp2 that stays in its place among its like
+__device__ __forceinline__ float exp2_in_order(float x)
+{
+    float r;
+    asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
 __device__ __forceinline__ uint32_t hmul2_u32(uint32_t a, uint32_t b)
@@ -488,6 +505,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
     unsigned long long* nan_s = reinterpret_cast<unsigned long long*>(smem + G::OFF_NAN);
     const uint32_t failed_at = sb + G::OFF_MISC;                 // word: a wait has given up
     uint32_t* tmem_s = reinterpret_cast<uint32_t*>(smem + G::OFF_MISC + 4);
+    const uint32_t finished_at = sb + G::OFF_MISC + 12;          // word: segments that the softmax warps are done with, summed
     volatile uint32_t* noted_s = reinterpret_cast<volatile uint32_t*>(smem + G::OFF_MISC + 8);    // segment of the latest note
     Share* share = reinterpret_cast<Share*>(smem + G::OFF_MISC + 16);
     // (the warp's number as a uniform value: whole-warp branches are then known as such)
@@ -499,11 +517,12 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
             int count = 1;
             if ((i >= kKFull && i < kKEmpty) || (i >= kVFull && i < kVEmpty) || i == kQFull) count = G::UNPACK_WARPS;
             else if (i >= kPFull && i < kPvDone) count = 4;
-            else if (i == kFacRead || i == kSegDone) count = G::SOFT_WARPS;
+            else if (i == kFacRead) count = G::SOFT_WARPS;
             mbar_init(bar(i), count);
         }
         sts32(failed_at, 0);
         *noted_s = 0;
+        sts32(finished_at, 0);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     for (int i = tid; i < D; i += G::THREADS) nan_s[i] = 0;
@@ -515,7 +534,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
         total *= P.hkv;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(FULL, total, o);
-        const long long per = max((total + gridDim.x - 1) / gridDim.x, (long long)(kLeastShare + kUnitCost));
+        const long long per = max((total + gridDim.x - 1) / gridDim.x, (long long)kLeastShare);
         const long long p0 = per * blockIdx.x;
         long long before = 0, at = 0;
         int found = -1;
@@ -560,26 +579,30 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
         __syncwarp();                                            // the segment before is no longer looked at
         bool more = false;
         if (lane == 0) more = walk->next<ROWS>(P, share);
+        __syncwarp();
         return __any_sync(FULL, more);
     };
 
     // Bounded by wall time: a wait that gives up flags the pool and lets every later wait of the block pass.  Polls are few
     // instructions, since they take issue slots from the working warps.
+    // The whole warp waits, and is in step again afterwards (what follows may be an instruction of the whole warp).
     auto wait = [&](int i, uint32_t parity) {
         const uint32_t a = bar(i);
-        if (mbar_try_wait(a, parity)) return;
-        unsigned long long t0 = 0, t1;
-        for (int polls = 1; !mbar_try_wait(a, parity); ++polls) {
-            __nanosleep(20);
-            if (polls & 63) continue;
-            if (lds32(failed_at)) return;
-            asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));
-            if (t0 == 0) t0 = t1;
-            if (t1 - t0 > P.wait_ns) {
-                sts32(failed_at, 1);
-                atomicOr(P.status, kStTimeout);
+        if (!mbar_try_wait(a, parity)) {
+            unsigned long long t0 = 0, t1;
+            for (int polls = 1; !mbar_try_wait(a, parity); ++polls) {
+                __nanosleep(20);
+                if (polls & 63) continue;
+                if (lds32(failed_at)) break;
+                asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));
+                if (t0 == 0) t0 = t1;
+                if (t1 - t0 > P.wait_ns) {
+                    sts32(failed_at, 1);
+                    atomicOr(P.status, kStTimeout);
+                }
             }
         }
+        __syncwarp();
     };
 
     if (warp >= G::MMA_WARP) {
@@ -591,25 +614,27 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
             while (next_segment()) {
                 const int nt = (int)uniform(s.nt), n = (int)uniform(s.t1 - s.t0) * nt;
                 const int turn = (int)uniform(max(s.u.stale_tiles - s.t0, 0));        // key tile of the segment that starts the FP8 ones
-                // job i of the segment: key tile t0 + i / nt, row tile i % nt; its scores are issued two jobs ahead
+                // job i of the segment: key tile t0 + i / nt, row tile i % nt; its scores are issued two jobs ahead.  With one row
+                // tile where there is room for two, the key tiles go by turns to two accumulators (and softmax groups).
+                const bool by_turns = NT == 2 && nt == 1;
                 for (int i = -2; i < n; ++i) {
                     if (i >= 0) {
-                        const uint32_t j = nt == 2 ? i >> 1 : i, t = nt == 2 ? i & 1 : 0;
+                        const uint32_t j = nt == 2 ? i >> 1 : i, t = NT == 2 ? i & 1 : 0;
                         const uint32_t at = tile + j, st = at % G::STAGES, buf = (job + i) & 1;
-                        if (t == 0) wait(kVFull + st, (at / G::STAGES) & 1);
+                        if (t == 0 || by_turns) wait(kVFull + st, (at / G::STAGES) & 1);
                         wait(kPFull + buf, ((job + i) >> 1) & 1);
                         tc_fence_after();
                         const uint64_t v = operand_desc(sb + G::OFF_V + st * G::V_TILE);
                         const uint32_t o = kTb + t * D, p = kTb + kColS + kKeys * buf;
 #pragma unroll
                         for (int kk = 0; kk < kKeys / 16; ++kk)
-                            issue_ts(o, p + 8 * kk, v + (((kk >> 2) * (D * 128) + (kk & 3) * 32) >> 4), idesc(D), kk > 0 ? 1u : (j > 0 ? 1u : 0u));
+                            issue_ts(o, p + 8 * kk, v + (((kk >> 2) * (D * 128) + (kk & 3) * 32) >> 4), idesc(D), kk > 0 ? 1u : (i >= NT ? 1u : 0u));
                         issue_commit(bar(kPvDone + t));
-                        if (i + nt >= n) issue_commit(bar(kOutput + t));
-                        if ((int)t == nt - 1) issue_commit(bar(kVEmpty + st));
+                        if (i + NT >= n) issue_commit(bar(kOutput + t));
+                        if (by_turns || (int)t == nt - 1) issue_commit(bar(kVEmpty + st));
                     }
                     if (i + 2 < n) {
-                        const uint32_t i2 = i + 2, j = nt == 2 ? i2 >> 1 : i2, t = nt == 2 ? i2 & 1 : 0;
+                        const uint32_t i2 = i + 2, j = nt == 2 ? i2 >> 1 : i2, t = NT == 2 && !by_turns ? i2 & 1 : 0;
                         const uint32_t at = tile + j, st = at % G::STAGES, buf = (job + i2) & 1;
                         if (t == 0) {
                             if (j == 0 || (int)j == turn) wait(kQFull, fills++ & 1);
@@ -666,12 +691,13 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
             const uint8_t* base3 = P.tq3 + s.h * page3;
 
             // ---- queries of one format: a warp per row, a lane D / 32 dims
-            auto fill_query = [&](bool stale) {
-                if (k_tile > 0) wait(kKEmpty + (k_tile - 1) % G::STAGES, ((k_tile - 1) / G::STAGES) & 1);   // the products so far are done
+            auto fill_query = [&](bool stale, uint32_t tiles) {  // tiles: key tiles whose products take the query before
+                if (tiles > 0) wait(kKEmpty + (tiles - 1) % G::STAGES, ((tiles - 1) / G::STAGES) & 1);
                 if (fills > 0) wait(kFacRead, (fills - 1) & 1);
                 ++fills;
                 constexpr int N = D / 32;
-                for (int r0 = w * 4; r0 < s.nt * 128; r0 += 4 * G::UNPACK_WARPS) {
+                // (rows behind the last one stay what they are: a row of a product sees no other)
+                for (int r0 = w * 4; r0 < ((rows + 31) & ~31); r0 += 4 * G::UNPACK_WARPS) {
                     uint32_t raw[4][N / 2];
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
@@ -772,7 +798,16 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
             // its bytes are cleared and the channel's first such position is noted; the epilogue gives NaN to the rows
             // from there on.  The note carries the segment, and the epilogue of the segment before is waited for.
             auto note_nan = [&](uint4 (&x)[16 * D / 512], int pos) {
-                if (segments > 1) wait(kSegDone, (segments - 2) & 1);
+                // (a count, not a barrier: the roles may be several segments apart)
+                unsigned long long t0, t1;
+                asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+                while (lds32(finished_at) < (segments - 1) * G::SOFT_WARPS && !lds32(failed_at)) {
+                    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));
+                    if (t1 - t0 > P.wait_ns) {
+                        sts32(failed_at, 1);
+                        atomicOr(P.status, kStTimeout);
+                    }
+                }
 #pragma unroll
                 for (int i = 0; i < 16 * D / 512; ++i) {
                     uint32_t* word = reinterpret_cast<uint32_t*>(&x[i]);
@@ -958,9 +993,12 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                 };
                 load_keys();
                 load_values();
-                fill_query(true);
-                put_keys();
-                load_keys();
+                {                                                // the first keys need not wait for the query's turn
+                    const uint32_t before = k_tile;
+                    put_keys();
+                    load_keys();
+                    fill_query(true, before);
+                }
                 for (int t = n_tiles - s.t0; t > 0; --t) {
                     if (t > 1) {
                         put_keys();
@@ -977,8 +1015,8 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                 // the run to load next (keys), looked up a tile ahead as above, and that of the tile before it (values)
                 const int last_page = (s.u.n_fp8 + P.tiles - 1) / P.tiles - 1;
                 Cursor kc;
-                uint2 k_page, v_page;
-                int k_sub, v_sub, k_left, v_left;
+                uint2 k_page, v_page = make_uint2(0, 0);
+                int k_sub, v_sub = 0, k_left, v_left = 0;
                 kc.open((t_first - cut) * 8 + w, s.u.n_fp8, P.tiles);
                 auto look = [&] {
                     k_page = ldg64(&list[P.max_pages - 1 - min(kc.page, last_page)]);
@@ -1076,9 +1114,12 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                 load_keys();
                 move_on();
                 load_values();
-                fill_query(false);
-                put_keys();
-                load_keys();
+                {                                                // the first keys need not wait for the query's turn
+                    const uint32_t before = k_tile;
+                    put_keys();
+                    load_keys();
+                    fill_query(false, before);
+                }
                 for (int t = s.t1 - t_first; t > 0; --t) {
                     move_on();
                     if (t > 1) {
@@ -1097,7 +1138,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
         const uint32_t my_lanes = (uint32_t)(32 * (warp & 3)) << 16;
         const int my_row = t * 128 + (warp & 3) * 32 + lane;     // within the unit
         const uint32_t col_o = tb + my_lanes + t * D;
-        uint32_t job = 0, fills = 0, done = 0, outputs = 0, segments = 0;   // done, outputs: value products, segments with any, on this row tile
+        uint32_t job = 0, fills = 0, done = 0, outputs = 0, joins = 0, segments = 0;   // done, outputs: value products, segments with any, on this row tile
         auto warp_arrive = [&](int i) {
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(i));
@@ -1119,28 +1160,32 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                 }
             };
             ++segments;
-            const int row = s.rt * ROWS + my_row, n_rows = s.r.n_new * P.group;
+            // one row tile where there is room for two: both groups take its rows, and the key tiles by turns
+            const bool by_turns = NT == 2 && s.nt == 1;
+            const int in_unit = my_row - (by_turns ? t * 128 : 0), row = s.rt * ROWS + in_unit, n_rows = s.r.n_new * P.group;
             const bool live = row < n_rows, warp_live = row - lane < n_rows;
             const int tok = row / P.group, head = s.h * P.group + row - tok * P.group;
             const int qpos = s.r.len - s.r.n_new + tok;
-            const int first_pos = s.r.len - s.r.n_new + (s.rt * ROWS + t * 128) / P.group;
+            const int first_pos = s.r.len - s.r.n_new + (s.rt * ROWS + (by_turns ? 0 : t * 128)) / P.group;
             const int2* list = P.list + (size_t)s.b * P.max_pages;
             const int cut = s.u.stale_tiles, runs = (s.r.len + 15) >> 4;
             const bool ordinary = s.r.exact && s.r.stale_end * kPage <= first_pos + 1;     // every Stale page lies before the first row
             float ref = -CUDART_INF_F, sum = 0.f, fac = 0.f;
             int n_done = 0;                                      // key tiles of this segment so far
+            bool in_stale = false;                               // the last one was a Stale tile
             const int t0 = s.t0, t1 = s.t1, nt = s.nt, n_stale = s.r.n_stale, n_fp8 = s.u.n_fp8, all_fp8 = s.r.n_fp8;
             for (int kt = t0; kt < t1; ++kt) {
                 const bool stale = kt < cut;
-                bool turn = false;                               // from Stale values' unit to the FP8 values'
                 if (kt == t0 || kt == cut) {
                     wait(kQFull, fills++ & 1);
-                    fac = fac_s[my_row];
+                    fac = fac_s[in_unit];
                     warp_arrive(kFacRead);
-                    turn = kt > t0 && P.v_scale != __uint_as_float((uint32_t)(127 + P.ve) << 23);
                 }
-                if (t >= nt) continue;
-                const uint32_t i = job + (uint32_t)(kt - t0) * nt + t, buf = i & 1;
+                if (by_turns ? ((kt - t0) & 1) != t : t >= nt) continue;
+                // from the Stale values' unit to the FP8 values'
+                const bool turn = !stale && in_stale && n_done > 0 && P.v_scale != __uint_as_float((uint32_t)(127 + P.ve) << 23);
+                in_stale = stale;
+                const uint32_t i = by_turns ? job + (uint32_t)(kt - t0) : job + (uint32_t)(kt - t0) * nt + t, buf = i & 1;
                 wait(kSFull + buf, (i >> 1) & 1);
                 tc_fence_after();
                 const uint32_t col_s = tb + my_lanes + kColS + kKeys * buf;
@@ -1217,17 +1262,31 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                         }
                         const float base = ref == -CUDART_INF_F ? 0.f : ref;
                         const float2 base2 = make_float2(-base, -base);
-                        float2 s2 = make_float2(0.f, 0.f);
+                        float2 s2[4];
                         uint32_t h2[COLS / 2];
+                        if constexpr (D == 256) {                // one warp a scheduler: in sweeps, no pair waits for its own steps
+#pragma unroll
+                            for (int k = 0; k < COLS; k += 2) {
+                                const float2 e = fma2(make_float2(x[k], x[k + 1]), fac2, base2);
+                                x[k] = e.x;
+                                x[k + 1] = e.y;
+                            }
+#pragma unroll
+                            for (int k = 0; k < COLS; ++k) x[k] = exp2_in_order(x[k]);
+                        }
 #pragma unroll
                         for (int k = 0; k < COLS / 2; ++k) {
-                            float2 e = fma2(make_float2(x[2 * k], x[2 * k + 1]), fac2, base2);
-                            e.x = fast_exp2(e.x);
-                            e.y = fast_exp2(e.y);
-                            s2 = add2(s2, e);
+                            float2 e = make_float2(x[2 * k], x[2 * k + 1]);
+                            if constexpr (D == 128) {
+                                e = fma2(e, fac2, base2);
+                                e.x = fast_exp2(e.x);
+                                e.y = fast_exp2(e.y);
+                            }
+                            s2[k & 3] = k < 4 ? e : add2(s2[k & 3], e);
                             h2[k] = pack_f16x2(e.x, e.y);
                         }
-                        sum += s2.x + s2.y;
+                        s2[0] = add2(add2(s2[0], s2[1]), add2(s2[2], s2[3]));
+                        sum += s2[0].x + s2[0].y;
                         tmem_st_n(col_s + COLS / 2 * c, h2);
                     }
                     tmem_wait_st();
@@ -1239,64 +1298,98 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
             }
             job += (uint32_t)(s.t1 - s.t0) * s.nt;
             if (n_done > 0) ++outputs;
-            if (t < s.nt && warp_live) {
+            if ((by_turns || t < s.nt) && warp_live) {
                 if (n_done > 0) {
                     wait(kOutput + t, (outputs - 1) & 1);
                     tc_fence_after();
                 }
-                // accumulators are in units of the last tile's values
-                const float unit = s.t1 > cut ? P.v_scale : __uint_as_float((uint32_t)(127 + P.ve) << 23);
-                const bool none = sum == 0.f, noted = *noted_s == segments;
-                const float f = s.slot >= 0 ? unit : none ? 0.f : unit / sum;
-                const size_t orow = (size_t)(s.r.row0 + tok) * (P.hkv * P.group) + head;
-                const size_t prow = (size_t)max(s.slot, 0) * ROWS + my_row;
-#pragma unroll 1
-                for (int c = 0; c < D / 32; ++c) {
-                    float x[32];
-                    if (n_done > 0) {
-                        tmem_ld32(col_o + 32 * c, x);
-                        tmem_wait_ld();
-                    }
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) x[k] = none || n_done == 0 ? 0.f : x[k] * f;
-                    if (noted) {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) {
-                            const unsigned long long note = nan_s[32 * c + k];
-                            if ((uint32_t)(note >> 32) == segments && kNoPos - (int)(uint32_t)note <= qpos) x[k] = CUDART_NAN_F;
-                        }
-                    }
-                    if (!live) continue;
-                    if (s.slot >= 0) {
-                        float4* dst = reinterpret_cast<float4*>(P.part_o + prow * D + 32 * c);
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) dst[k] = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+                // by turns: the first group joins both (the second one's reference, sum and unit come through shared memory; its
+                // accumulator has the same lanes)
+                float join = 0.f;                                // factor of the second accumulator
+                int n_join = 0;                                  // key tiles in it (of the whole warp: it decides on loads)
+                float unit = in_stale ? __uint_as_float((uint32_t)(127 + P.ve) << 23) : P.v_scale;    // of the accumulator: the last tile's
+                if (by_turns) {
+                    const uint32_t at = sb + G::OFF_PAIR + 16 * in_unit;
+                    if (t == 1) {
+                        sts128(at, __float_as_uint(ref), __float_as_uint(sum), __float_as_uint(unit), 0);
+                        tc_fence_before();
+                        warp_arrive(kJoin + (warp & 3));
                     } else {
-                        uint4* dst = reinterpret_cast<uint4*>(P.out + orow * D + 32 * c);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            uint32_t o[4];
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                const __nv_bfloat162 p2 = __floats2bfloat162_rn(x[8 * k + 2 * q], x[8 * k + 2 * q + 1]);
-                                o[q] = *reinterpret_cast<const uint32_t*>(&p2);
-                            }
-                            dst[k] = make_uint4(o[0], o[1], o[2], o[3]);
-                        }
+                        wait(kJoin + (warp & 3), joins & 1);
+                        tc_fence_after();
+                        n_join = (t1 - t0) >> 1;
+                        const uint4 o = lds128(at);
+                        const float ref1 = __uint_as_float(o.x), sum1 = __uint_as_float(o.y), to = fmaxf(ref, ref1);
+                        const float f0 = ref == -CUDART_INF_F ? sum : exp2f(ref - to);       // no maximum: nothing, or NaN
+                        const float f1 = ref1 == -CUDART_INF_F ? sum1 : exp2f(ref1 - to);
+                        sum = sum * f0 + sum1 * f1;
+                        unit *= f0;
+                        join = f1 * __uint_as_float(o.z);
+                        ref = to;
                     }
                 }
-                if (live) {
-                    if (s.slot >= 0) P.part_ml[prow] = make_float2(ref, sum);
-                    else if (P.lse) P.lse[orow] = none ? -CUDART_INF_F : (ref + log2f(sum)) * 0.6931471805599453f;
+                if (t == 0 || !by_turns) {                       // this group writes the rows
+                    const bool none = sum == 0.f, noted = *noted_s == segments;
+                    const float f = s.slot >= 0 ? unit : none ? 0.f : unit / sum, f1 = s.slot >= 0 ? join : none ? 0.f : join / sum;
+                    const size_t orow = (size_t)(s.r.row0 + tok) * (P.hkv * P.group) + head;
+                    const size_t prow = (size_t)max(s.slot, 0) * ROWS + in_unit;
+#pragma unroll 1
+                    for (int ch = 0; ch < D; ch += 16) {
+                        float x[16], y[16];
+                        if (n_done > 0) tmem_ld_n(col_o + ch, x);
+                        if (NT == 2 && n_join > 0) tmem_ld_n(col_o + D + ch, y);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            x[k] = none || n_done == 0 ? 0.f : x[k] * f;
+                            if (NT == 2 && n_join > 0) x[k] = f1 == 0.f ? x[k] : fmaf(y[k], f1, x[k]);
+                        }
+                        if (noted) {
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) {
+                                const unsigned long long note = nan_s[ch + k];
+                                if ((uint32_t)(note >> 32) == segments && kNoPos - (int)(uint32_t)note <= qpos) x[k] = CUDART_NAN_F;
+                            }
+                        }
+                        if (live && s.slot >= 0) {
+                            float4* dst = reinterpret_cast<float4*>(P.part_o + prow * D + ch);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) dst[k] = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+                        } else if (live) {
+                            uint4* dst = reinterpret_cast<uint4*>(P.out + orow * D + ch);
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                uint32_t o[4];
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) {
+                                    const __nv_bfloat162 p2 = __floats2bfloat162_rn(x[8 * k + 2 * q], x[8 * k + 2 * q + 1]);
+                                    o[q] = *reinterpret_cast<const uint32_t*>(&p2);
+                                }
+                                dst[k] = make_uint4(o[0], o[1], o[2], o[3]);
+                            }
+                        }
+                        __syncwarp();
+                    }
+                    if (live) {
+                        if (s.slot >= 0) P.part_ml[prow] = make_float2(ref, sum);
+                        else if (P.lse) P.lse[orow] = none ? -CUDART_INF_F : (ref + log2f(sum)) * 0.6931471805599453f;
+                    }
                 }
                 tc_fence_before();
+                if (by_turns) {                                  // the second accumulator has been read
+                    if (t == 0) warp_arrive(kJoined + (warp & 3));
+                    else wait(kJoined + (warp & 3), joins & 1);
+                    ++joins;
+                }
             }
             if (s.first_part && tid == 0) {
                 Merge m = {};
                 m.b = s.b; m.h = s.h; m.rt = s.rt; m.last = s.last_block; m.first_slot = s.slot;
                 P.merge[blockIdx.x] = m;
             }
-            warp_arrive(kSegDone);
+            __threadfence_block();
+            __syncwarp();
+            if (lane == 0) atomicAdd(reinterpret_cast<uint32_t*>(smem + G::OFF_MISC + 12), 1u);
         }
     }
     __syncthreads();
