@@ -323,6 +323,9 @@ struct Turn {
     float c[8], s[8];
 };
 
+// half turns in [-1, 1): the angle's top 32 bits
+__device__ __forceinline__ float half_turns(unsigned long long f) { return (float)(int)(f >> 32) * 4.656612873077393e-10f; }
+
 __device__ __forceinline__ void turn_of(Turn& t, const RotaryArgs& A, int token, int u)
 {
     // top 32 bits of the angles first: their loads wait for one another, the sines need none
@@ -342,7 +345,7 @@ __device__ __forceinline__ void turn_of(Turn& t, const RotaryArgs& A, int token,
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        sincospif((float)top[i] * 4.656612873077393e-10f, &t.s[i], &t.c[i]);            // 2^-31: half turns
+        sincospif(half_turns((unsigned long long)(uint32_t)top[i] << 32), &t.s[i], &t.c[i]);
         t.c[i] *= A.mscale;
         t.s[i] *= A.mscale;
     }
@@ -422,46 +425,68 @@ __device__ __forceinline__ void unit_dims(const RotaryArgs& A, int u, int& lo, i
     hi = apart ? 8 * A.units + 8 * u : lo + 8;
 }
 
-// Decode-sized calls: a block per (token, KV head), a thread per unit of one of its query heads, its key or its value.
-// Bound by latency: position, slot, inputs and frequencies are loaded at once, sines and stores follow.
+// Decode-sized calls: a block per (token, KV head); two channels of its value to a thread, then a unit of its query heads
+// or its key to a thread.  Bound by latency: inputs, position, slot and frequencies are loaded at once, the block's sines
+// are shared out and meet in shared memory.
 template <int D, bool INTERLEAVED>
-__global__ void __launch_bounds__((kMaxGroup + 2) * D / 16) append_rotary_kernel(const RotaryArgs A)
+__global__ void __launch_bounds__((kMaxGroup + 1) * D / 16 + D / 2) append_rotary_kernel(const RotaryArgs A)
 {
+    __shared__ __align__(16) float cos_s[D / 2], sin_s[D / 2];
     pdl_begin();
-    const int tok = blockIdx.x, h = blockIdx.y, u = threadIdx.x % (D / 16), item = threadIdx.x / (D / 16);
-    const int n_q = A.q ? A.group : 0;                       // items: query heads, then key, then value
-    const bool is_q = item < n_q, is_v = item == n_q + 1;
-    float x[16];
+    const int tok = blockIdx.x, h = blockIdx.y, n_v = A.k ? D / 2 : 0, at = (int)threadIdx.x - n_v;
+    const int u = at & (D / 16 - 1), item = at / (D / 16), n_q = A.q ? A.group : 0;       // items: query heads, then the key
+    const bool is_v = at < 0, is_q = !is_v && item < n_q;
     int lo, hi;
     unit_dims<INTERLEAVED>(A, u, lo, hi);
-    if (is_v) { lo = 16 * u; hi = lo + 8; }
-    const uint16_t* src = is_q ? A.q + (size_t)tok * A.q_stride + (size_t)(h * A.group + item) * D
-                               : (is_v ? A.v + (size_t)tok * A.v_stride : A.k + (size_t)tok * A.k_stride) + (size_t)h * D;
-    load_unit(x, src + lo, src + hi);
+    Raw raw = {};
+    __nv_bfloat162 v2 = {};
+    if (is_v) v2 = *reinterpret_cast<const __nv_bfloat162*>(A.v + (size_t)tok * A.v_stride + (size_t)h * D + 2 * threadIdx.x);
+    else {
+        const uint16_t* src = is_q ? A.q + (size_t)tok * A.q_stride + (size_t)(h * A.group + item) * D
+                                   : A.k + (size_t)tok * A.k_stride + (size_t)h * D;
+        raw = load_raw(src + lo, src + hi);
+    }
     const int slot = is_q ? -1 : A.slots[tok];
-    if (!is_v && u < A.units) {
+    for (int j = threadIdx.x; j < 8 * A.units; j += blockDim.x) {
+        const int p = A.positions[A.axis ? (size_t)min((int)A.axis[j], A.n_axes - 1) * A.n + tok : (size_t)tok];
+        float s, c;
+        sincospif(half_turns((unsigned long long)(long long)p * A.turns[j]), &s, &c);
+        cos_s[j] = c * A.mscale;
+        sin_s[j] = s * A.mscale;
+    }
+    uint8_t* rec = record_of<D>(A, slot, h, is_v && threadIdx.x == 0);
+    if (is_v && rec) {                                       // channel-major
+        float2 f = __bfloat1622float2(v2);
+        f.x = __fmul_rn(f.x, A.inv_v_scale);
+        f.y = __fmul_rn(f.y, A.inv_v_scale);
+        const __nv_fp8x2_storage_t two = __nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
+        uint8_t* ch = rec + 16 * D + 2 * threadIdx.x * kPage + (slot & 15);
+        ch[0] = (uint8_t)(two & 0xFF);
+        ch[kPage] = (uint8_t)(two >> 8);
+    }
+    __syncthreads();
+    if (is_v) return;
+    float x[16];
+    to_fp32(x, raw);
+    if (u < A.units) {
         Turn t;
-        turn_of(t, A, tok, u);
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+            const float4 c = *reinterpret_cast<const float4*>(cos_s + 8 * u + i), s = *reinterpret_cast<const float4*>(sin_s + 8 * u + i);
+            t.c[i] = c.x; t.c[i + 1] = c.y; t.c[i + 2] = c.z; t.c[i + 3] = c.w;
+            t.s[i] = s.x; t.s[i + 1] = s.y; t.s[i + 2] = s.z; t.s[i + 3] = s.w;
+        }
         turn_unit<INTERLEAVED>(x, t);
     }
     if (is_q) {
         uint16_t* dst = A.q_out + (size_t)tok * A.out_stride + (size_t)(h * A.group + item) * D;
         *reinterpret_cast<uint4*>(dst + lo) = to_bf16x8(x);
         *reinterpret_cast<uint4*>(dst + hi) = to_bf16x8(x + 8);
-        return;
-    }
-    uint8_t* rec = record_of<D>(A, slot, h, u == 0 && !is_v);
-    if (!rec) return;
-    const uint2 a = to_e4m3x8(x, is_v ? A.inv_v_scale : A.inv_k_scale), b = to_e4m3x8(x + 8, is_v ? A.inv_v_scale : A.inv_k_scale);
-    if (!is_v) {
+    } else if (rec) {
         uint8_t* row = rec + (slot & 15) * D;
-        *reinterpret_cast<uint2*>(row + lo) = a;
-        *reinterpret_cast<uint2*>(row + hi) = b;
-        return;
+        *reinterpret_cast<uint2*>(row + lo) = to_e4m3x8(x, A.inv_k_scale);
+        *reinterpret_cast<uint2*>(row + hi) = to_e4m3x8(x + 8, A.inv_k_scale);
     }
-    const uint32_t w[4] = {a.x, a.y, b.x, b.y};
-#pragma unroll
-    for (int i = 0; i < 16; ++i) rec[16 * D + (lo + i) * kPage + (slot & 15)] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
 }
 
 // Prefill-sized calls: a block per (window of 16 tokens, KV head), a thread per (token, unit): its sines serve the key and
@@ -557,8 +582,8 @@ static int32_t launch_rotary(const RotaryArgs& A, cudaStream_t s)
     if (A.n >= kAppendRun)
         MKV_CUDA(launch_pdl(append_rotary_run_kernel<D, INTERLEAVED>, dim3((A.n + kPage - 1) / kPage, A.hkv), D, 0, 1, s, A));
     else
-        MKV_CUDA(launch_pdl(append_rotary_kernel<D, INTERLEAVED>, dim3(A.n, A.hkv), ((A.q ? A.group : 0) + (A.k ? 2 : 0)) * D / 16, 0, 1,
-                            s, A));
+        MKV_CUDA(launch_pdl(append_rotary_kernel<D, INTERLEAVED>, dim3(A.n, A.hkv),
+                            ((A.q ? A.group : 0) + (A.k ? 1 : 0)) * D / 16 + (A.k ? D / 2 : 0), 0, 1, s, A));
     MKV_CUDA(cudaGetLastError());
     return MKV_OK;
 }
