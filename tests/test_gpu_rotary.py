@@ -76,8 +76,20 @@ CASES = [  # d, hkv, group, rotary_dim, axes, interleaved
 
 @gpu
 @pytest.mark.parametrize("d,hkv,group,rotary_dim,n_axes,interleaved", CASES)
-@pytest.mark.parametrize("n,page", [(1, 16), (2, 16), (37, 48), (255, 16), (256, 16), (271, 16), (700, 48), (1300, 832)])
+@pytest.mark.parametrize("n,page", [(1, 16), (2, 16), (37, 48), (255, 16), (256, 16), (271, 16), (700, 48), (1300, 832), (2300, 48)])
 def test_against_the_rotation_in_64_bits(d, hkv, group, rotary_dim, n_axes, interleaved, n, page):
+    check_case(d, hkv, group, rotary_dim, n_axes, interleaved, n, page)
+
+
+@gpu
+@pytest.mark.parametrize("d,hkv,group,rotary_dim,n_axes,interleaved,n,page", [
+    (128, 1, 8, 64, 1, True, 9000, 16), (256, 1, 5, 96, 3, False, 4203, 48), (128, 3, 1, 16, 2, False, 2800, 16),
+    (128, 2, 1, 128, 1, False, 4096, 16), (128, 2, 3, 128, 1, False, 4095, 16)])
+def test_prompts_of_few_heads(d, hkv, group, rotary_dim, n_axes, interleaved, n, page):
+    check_case(d, hkv, group, rotary_dim, n_axes, interleaved, n, page)
+
+
+def check_case(d, hkv, group, rotary_dim, n_axes, interleaved, n, page):
     rng = np.random.RandomState(n + d + rotary_dim)
     pages = n // page * 3 + n // 4 + 4
     k_scale, v_scale, mscale = 0.5, 2.0, 1.25 if n % 2 else 1.0
@@ -118,12 +130,12 @@ def test_against_the_rotation_in_64_bits(d, hkv, group, rotary_dim, n_axes, inte
 
 
 @gpu
-@pytest.mark.parametrize("n", [5, 400])
+@pytest.mark.parametrize("n", [5, 400, 4200])
 def test_keys_only_and_queries_only(n):
     rng = np.random.RandomState(n)
     inv = frequencies(64)
     rot = M.Rotary(inv)
-    a, b, c = (M.Pool(128, 2, 4, 40, 1, np.ones(128, np.int8)) for _ in range(3))
+    a, b, c = (M.Pool(128, 2, 4, n // 16 + 15, 1, np.ones(128, np.int8)) for _ in range(3))
     q, k, v = (torch.from_numpy(rng.randn(n, h, 128).astype(np.float32)).bfloat16().cuda() for h in (4, 2, 2))
     slots = torch.arange(n, dtype=torch.int32, device="cuda")
     pos = torch.arange(n, dtype=torch.int32, device="cuda") + 77
@@ -135,22 +147,23 @@ def test_keys_only_and_queries_only(n):
 
 
 @gpu
-@pytest.mark.parametrize("n", [20, 300])
+@pytest.mark.parametrize("n", [20, 300, 8300])
 def test_slots_beyond_the_store_are_flagged_and_saturation_and_nan(n):
-    pool = M.Pool(128, 1, 1, 30, 1, np.ones(128, np.int8))
+    pages = max(30, n // 16 + 2)
+    pool = M.Pool(128, 1, 1, pages, 1, np.ones(128, np.int8))
     q, k, v = (torch.ones(n, 1, 128, dtype=torch.bfloat16, device="cuda") for _ in range(3))
     k[0], k[1, 0, 5], v[2] = 1e6, float("nan"), -1e6
     slots = torch.arange(n, dtype=torch.int32, device="cuda")
-    slots[n - 1] = 30 * 16
+    slots[n - 1] = pages * 16
     slots[n - 2] = (1 << 31) - 1
     pos = torch.zeros(n, dtype=torch.int32, device="cuda")
     rot = M.Rotary(frequencies(64))
     pool.append_rotary(q, k, v, slots, pos, rot)
     assert pool.status() == M.E_BOUNDS and pool.status() == M.OK
-    rec = pool.fp8_arena[:30 * 4096].view(30, 4096).view(torch.float8_e4m3fn).float()
+    rec = pool.fp8_arena[:pages * 4096].view(pages, 4096).view(torch.float8_e4m3fn).float()
     assert (rec[0, :128] == 448).all() and rec[0, 128 + 5].isnan() and (rec[0, 2048 + 2::16] == -448).all()
     written = rec[:, :2048].reshape(-1, 128)
-    assert (written[2:n - 2] == 1).all() and not written[n - 2:480].any()
+    assert (written[2:n - 2] == 1).all() and not written[n - 2:].any()
 
 
 @gpu
