@@ -26,6 +26,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math_constants.h>
+#include <mutex>
 
 #include "mkv_internal.cuh"
 #include "tensor_ptx.cuh"
@@ -236,14 +237,18 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const Params P
     __syncthreads();
     for (int base = 0; base < pages; base += kPlanThreads * kPlanPer) {
         const int p0 = base + tid * kPlanPer;
-        int id[kPlanPer];
+        int id[kPlanPer], tag_of[kPlanPer];
         uint32_t stale = 0, fp8 = 0;
 #pragma unroll
-        for (int i = 0; i < kPlanPer; ++i) {
-            const int p = p0 + i;
-            if (p >= pages) break;
-            const int tag = tags[p];
+        for (int i = 0; i < kPlanPer; ++i) {                    // (all at once: no load waits for another)
+            const int p = min(p0 + i, pages - 1);
+            tag_of[i] = tags[p];
             id[i] = ids[p];
+        }
+#pragma unroll
+        for (int i = 0; i < kPlanPer; ++i) {
+            const int p = p0 + i, tag = tag_of[i];
+            if (p >= pages) continue;
             const bool is_stale = tag == MKV_TAG_STALE;
             const bool ok = is_stale ? id[i] >= 0 && id[i] < P.tq3_pages && (long long)(p + 1) * T <= len
                                      : tag <= MKV_TAG_ANCHOR && id[i] >= 0 && id[i] < P.fp8_pages;
@@ -1307,6 +1312,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                 // accumulator has the same lanes)
                 float join = 0.f;                                // factor of the second accumulator
                 int n_join = 0;                                  // key tiles in it (of the whole warp: it decides on loads)
+                bool joins_in = false;                           // the row sees any of them
                 float unit = in_stale ? __uint_as_float((uint32_t)(127 + P.ve) << 23) : P.v_scale;    // of the accumulator: the last tile's
                 if (by_turns) {
                     const uint32_t at = sb + G::OFF_PAIR + 16 * in_unit;
@@ -1325,6 +1331,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                         sum = sum * f0 + sum1 * f1;
                         unit *= f0;
                         join = f1 * __uint_as_float(o.z);
+                        joins_in = f1 != 0.f || ref1 != -CUDART_INF_F;
                         ref = to;
                     }
                 }
@@ -1342,7 +1349,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
                             x[k] = none || n_done == 0 ? 0.f : x[k] * f;
-                            if (NT == 2 && n_join > 0) x[k] = f1 == 0.f ? x[k] : fmaf(y[k], f1, x[k]);
+                            if (NT == 2 && n_join > 0) x[k] = joins_in ? fmaf(y[k], f1, x[k]) : x[k];
                         }
                         if (noted) {
 #pragma unroll
@@ -1464,17 +1471,30 @@ static Layout layout_of(int d, int B, int max_pages)
 }
 
 template <int D, int FMT>
-static int32_t launch(const Params& P, int sms, cudaStream_t s)
+static int32_t launch(const Params& P, int device, int sms, cudaStream_t s)
 {
     using G = Geo<D>;
-    // the warps' shares of the registers add up to the launch's: a build that takes fewer would wait for the rest for ever
-    cudaFuncAttributes attr;
-    MKV_CUDA(cudaFuncGetAttributes(&attr, chunk_scan_kernel<D, FMT>));
-    if (attr.numRegs != G::REGS) {
-        set_last_error("chunk attention: the kernel was built with another number of registers than its warps share out");
-        return MKV_E_CUDA;
+    // once per device: the kernel's shared memory, and a check that the warps' shares of the registers add up to the launch's (a
+    // build that takes fewer would wait for the rest for ever)
+    static std::mutex mu;
+    static unsigned long long ready = 0;                         // a bit per device
+    {
+        std::lock_guard<std::mutex> lk(mu);
+        if (device < 0 || device >= 64) {
+            set_last_error("chunk attention: device index beyond the 64 this library keeps launch state for");
+            return MKV_E_INVALID;
+        }
+        if (!(ready >> device & 1)) {
+            cudaFuncAttributes attr;
+            MKV_CUDA(cudaFuncGetAttributes(&attr, chunk_scan_kernel<D, FMT>));
+            if (attr.numRegs != G::REGS) {
+                set_last_error("chunk attention: the kernel was built with another number of registers than its warps share out");
+                return MKV_E_CUDA;
+            }
+            MKV_CUDA(cudaFuncSetAttribute(chunk_scan_kernel<D, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM));
+            ready |= 1ull << device;
+        }
     }
-    MKV_CUDA(cudaFuncSetAttribute(chunk_scan_kernel<D, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM));
     if ((unsigned long long)P.hkv * fp8_page_bytes(D, P.tiles) >> 32) {
         set_last_error("chunk attention: a page of all KV heads has 4 GB or more");
         return MKV_E_INVALID;
@@ -1528,8 +1548,8 @@ int32_t launch_chunk_attention(mkv_pool* p, const void* q, int64_t q_stride, int
     P.status = p->status_dev;
     P.wait_ns = p->wait_ns;
     const int sms = p->dev.sm_count;
-    if (p->d == 128) return p->fmt == 2 ? launch<128, 2>(P, sms, s) : launch<128, 1>(P, sms, s);
-    return p->fmt == 2 ? launch<256, 2>(P, sms, s) : launch<256, 1>(P, sms, s);
+    if (p->d == 128) return p->fmt == 2 ? launch<128, 2>(P, p->device, sms, s) : launch<128, 1>(P, p->device, sms, s);
+    return p->fmt == 2 ? launch<256, 2>(P, p->device, sms, s) : launch<256, 1>(P, p->device, sms, s);
 }
 
 }  // namespace mkv

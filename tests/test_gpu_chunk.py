@@ -414,3 +414,49 @@ def test_refusals_on_a_device_pool():
     assert (out == 2).all() and pool.status() == M.OK
     empty = pool.chunk_attention(q[:0], torch.zeros(2, dtype=torch.int32, device="cuda"), table, tags, lens, 0.1)
     assert empty.shape == (0, 4, 128)
+
+
+@gpu
+@pytest.mark.parametrize("d,group", [(128, 4), (128, 8), (256, 6)])
+def test_many_calls_give_the_same_bits(d, group):
+    """Units of every size, 200 calls in a row on one workspace and on two streams with a workspace each."""
+    c = Cache(d, 2, group, [(517, 1), (1030, 5), (300, 40), (700, 33), (1, 1), (0, 3), (140, 140)], 2, seed=61, stale=0.6)
+    pool, dev, q = c.pool(), c.device(), c.q.cuda()
+    ws = [pool.chunk_workspace(7, c.table.shape[1]) for _ in range(2)]
+    want = pool.chunk_attention(q, *dev, c.scale, out=torch.empty_like(q), workspace=ws[0])
+    outs = [torch.zeros_like(q) for _ in range(8)]
+    different = torch.zeros((), dtype=torch.int64, device="cuda")
+    for i in range(200):
+        pool.chunk_attention(q, *dev, c.scale, out=outs[i % 8], workspace=ws[0])
+        if i % 8 == 7:
+            different += sum((o != want).sum() for o in outs)
+    streams = [torch.cuda.Stream() for _ in ws]
+    torch.cuda.synchronize()
+    for i in range(60):
+        for k, s in enumerate(streams):
+            pool.chunk_attention(q, *dev, c.scale, out=outs[4 * k + i % 4], workspace=ws[k], stream=s)
+    torch.cuda.synchronize()
+    different += sum((o != want).sum() for o in outs)
+    assert different.item() == 0 and pool.status() == M.OK
+
+
+@gpu
+@pytest.mark.parametrize("d,group", [(128, 2), (128, 8), (256, 3)])
+def test_nan_in_several_units_of_a_block(d, group):
+    """NaN values in the chunks of many short requests: every block meets several such units one behind the other."""
+    rng = np.random.RandomState(4)
+    c = Cache(d, 4, group, [(int(n), int(min(n, 3 + n % 20))) for n in rng.randint(20, 200, 160)], 1, seed=71, stale=0.3)
+    marks = []
+    for b in range(0, 160, 2):
+        token = int(c.lens[b] - c.new[b]) + b % int(c.new[b])          # a token of the chunk: rows before it do not see it
+        page, at, h, ch = c.table[b, token // 16], token % 16, b % 4, (7 * b) % d
+        c.fp8[page, h, 16 * d:].reshape(d, 16)[ch, at] = 0x7F
+        marks.append((int(c.starts[b]) + b % int(c.new[b]), int(c.starts[b + 1]), h, ch))
+    want = torch.zeros(c.q.shape, dtype=torch.bool)
+    for r0, r1, h, ch in marks:
+        want[r0:r1, h * group:(h + 1) * group, ch] = True
+    for _ in range(3):
+        out, lse, pool = run(c)
+        assert pool.status() == M.OK and torch.equal(out.isnan().cpu(), want) and lse.isfinite().all()
+    ref = c.reference()
+    c.check(torch.where(want.cuda(), torch.from_numpy(ref[0]).cuda().bfloat16(), out), lse, ref)
