@@ -199,8 +199,8 @@ int32_t mkv_append(mkv_pool* pool, const void* k_dev, const void* v_dev, const i
  *   slot_mapping device, int32 [n], as mkv_append: a negative slot stores nothing (its query is turned all the same); two
  *                tokens with the same slot: which of them stays is not defined
  *   positions    device, int32 [n_axes][n]
- *   q_out        device, bf16, out_stride elements from a token to the next; may be q itself with q's stride, and must
- *                not overlap it otherwise */
+ *   q_out        device, bf16, out_stride elements from a token to the next; may be q itself with q's stride, and shares no
+ *                row with q, k or v otherwise (MKV_E_INVALID; another slice of the same buffer is fine) */
 typedef struct {
     const uint64_t* turns_dev;
     const uint8_t* axis_dev;
@@ -365,14 +365,16 @@ int32_t mkv_decode_attention_scored(mkv_pool* pool, const void* q_dev, const int
  *                invalid entry skipped and recorded; a Stale page that is not full is invalid)
  *   scale        finite; may be 0 or negative
  *   out          device, bf16 [n_rows][n_q_heads][d], dense.  A row that sees nothing (its position is negative, or all
- *                its pages invalid) is 0 with lse = -inf
+ *                its pages invalid) is 0 with lse = -inf.  Must not overlap q (MKV_E_INVALID)
  *   lse          device, fp32 [n_rows][n_q_heads], natural logarithm, or NULL
  *   workspace    device, at least mkv_chunk_workspace_bytes(cfg, B, max_pages) bytes, 256-byte aligned, any contents; two
  *                calls that overlap on the GPU need two buffers
  * Keys, values and probabilities enter the tensor core as fp16 (FP8 pages exactly) and are summed in fp32: out is within
  * a bf16 rounding and about 1e-3 of the exact result, lse within about 1e-3.  Values are held relative to a power of two near
- * the pool's scales, so that whatever Demote writes fits.  NaN in a key or value reaches the rows that see it, and no
- * others.  Three launches; results do not depend on what else runs.  No host synchronisation. */
+ * the pool's scales, so that whatever Demote writes fits: norms, scales and zeros of Stale pages are taken to be finite, as
+ * Demote writes them.  NaN in a key or value of an FP8 page reaches the rows that see it, and no others.  Pools whose pages
+ * (all KV heads) have 4 GB or more are refused.  Three launches; the same call gives the same bits.  No host
+ * synchronisation. */
 int32_t mkv_chunk_workspace_bytes(const mkv_pool_config* cfg, int32_t max_batch, int32_t max_pages, size_t* bytes);
 int32_t mkv_chunk_attention(mkv_pool* pool, const void* q_dev, int64_t q_stride, int32_t n_rows, const int32_t* q_starts_dev,
                             const int32_t* block_table_dev, const uint8_t* tier_tag_dev, const int32_t* seq_lens_dev, int32_t B,

@@ -460,7 +460,7 @@ class Pool:
         tensors = [q, q_starts, block_table, tier_tag, seq_lens, out, workspace] + ([lse] if lse is not None else [])
         assert all(t.device == self.fp8_arena.device for t in tensors), "every tensor is on the pool's device"
         with torch.cuda.device(self.fp8_arena.device):
-            _check(lib().mkv_chunk_attention(self.handle, _ptr(q), q.stride(0), n, _ptr(q_starts), _ptr(block_table), _ptr(tier_tag),
+            _check(lib().mkv_chunk_attention(self.handle, _ptr(q), q.stride(0) if n > 1 else self.hq * self.d, n, _ptr(q_starts), _ptr(block_table), _ptr(tier_tag),
                                              _ptr(seq_lens), B, block_table.shape[1], float(scale), _ptr(out), _ptr(lse),
                                              _ptr(workspace), workspace.numel(), _stream(stream)), "mkv_chunk_attention")
         return out

@@ -9,6 +9,8 @@
 //   * The rows of a tile are (token, query head) pairs of one KV head, 128 per tensor-memory accumulator: a query group
 //     shares every unpacked key and value.  A block takes two such row tiles at d = 128 and one at d = 256 (the output
 //     accumulators, 256 columns, and two score buffers of 128 columns fill tensor memory) and walks tiles of 128 keys.
+//     Where a unit fills one of two row tiles, the key tiles go by turns to both accumulators (8 requests of 5 rows over 16K
+//     tokens, d = 128: 89 us with one, 77 by turns).
 //   * Each key tile holds pages of one format (chunk_plan_kernel sorts a row's pages by format), so that the products
 //     take one query: the rotated one for Stale tiles, then the plain one, written over it, for FP8 tiles.
 //   * Pages are unpacked once per block to fp16 in shared memory, K-major with the 128-byte swizzle, by eight warps
@@ -16,13 +18,26 @@
 //     element on average, as the probabilities' rounding and far below the output's bf16).  A lane of the packed
 //     fragment order holds scattered dims (keys) and tokens (values): the order of the contraction is free, so query dims
 //     and key rows are permuted such that every lane's share is one 16-byte store without bank conflicts.
-//   * One thread issues the products S = Q K^T (both operands in shared memory) and O += P V (P in tensor memory, over
+//   * One warp issues the products S = Q K^T (both operands in shared memory) and O += P V (P in tensor memory, over
 //     the scores it came from), the scores of the tile after next before the softmax of this one has finished.
 //   * A softmax thread owns a row (its tensor-memory lane): no exchange between threads.  The reference of the
 //     exponentials is raised only when a score exceeds it by 2^15, which keeps P within fp16 and rescaling of O rare;
 //     it lies 7 below the maximum, so that probabilities down to 2^-31 of the largest are not flushed.
 //   * (unit, key tiles) pairs are cut evenly over the SMs; a unit that several blocks share leaves fp32 partials
 //     (m, l, O) in the workspace and chunk_merge_kernel joins them (Eq. softmax-merge), in the order of the blocks.
+//
+// What bounds it (B200; measured with the arenas in HBM, rates are of the visible pairs' 4 d flops):
+//   * Long chunks, d = 256 (2,048 rows of 24 heads over 57K tokens, format 2): 2.9 ms, 1.0 PFLOP/s, 60 % of what a large bf16
+//     matrix product reaches here.  The data path of shared memory is 80 % busy: unpacked tiles are stored and then read by
+//     the products of one row tile; unpacking left out, it would be 2.3 ms.  Sharing a tile between two SMs would halve that.
+//   * d = 128 (1,000 rows of 32 heads over 16K tokens, twice): 0.8 ms, 0.69 PFLOP/s.  The softmax: 128 columns take a warp 2,000
+//     cycles alone, 3,200 with a second one on its scheduler, 4,600 with two unpacking warps besides.  Score buffers of 64 columns,
+//     four of them, hide the wait for the scores and lose more in steps (0.9 ms); two threads to a row, the softmax fully unrolled,
+//     wider tensor-memory loads (registers) and unpacking split by keys and values were slower, too.
+//   * Prompts (3 x 4,097 rows, d = 256): 0.75 ms, half of the rate: the causal half of the last tiles is masked, and a unit's query
+//     and epilogue cost as much as six key tiles.
+//   * A few rows per request: latency.  4 rows over 4,092 tokens: 29 us in three launches, of which the plan takes 4, the scan's start
+//     (share, query, first keys) 6, its two tiles 5, partials and merge 7.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math_constants.h>
@@ -36,8 +51,10 @@ namespace chunk {
 
 constexpr int kMaxBlocks = 160;              // of the scan's grid: sizes the partials
 constexpr int kKeys = 128;                   // keys of a tile: eight runs of 16 tokens
-constexpr int kUnitCost = 6;                 // what a unit costs besides its key tiles (query, epilogue), in key tiles
-constexpr int kLeastShare = 2;               // key tiles of a block at least
+// What a unit costs besides its key tiles (query, epilogue), in key tiles: 3 prompts of 4,097 tokens 0.75 ms with 6 and 8, 0.89
+// with 2; 16 mixed requests 0.35 and 0.43.
+constexpr int kUnitCost = 6;
+constexpr int kLeastShare = 2;               // of a block, in key tiles: smaller shares cost more in partials than they save
 constexpr float kShift = 7.f, kSlack = 8.f;  // see above: probabilities are at most 2^(kShift + kSlack)
 constexpr int kNoPos = 0x7fffffff;
 
@@ -413,7 +430,8 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
         : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
     return r;
 }
-// fast_exp2 that stays in its place among its like
+// fast_exp2 that stays in its place among its like (a lone warp on a scheduler, d = 256, then runs its exponentials in one sweep;
+// with two warps, d = 128, the compiler's order is as fast and takes fewer registers)
 __device__ __forceinline__ float exp2_in_order(float x)
 {
     float r;

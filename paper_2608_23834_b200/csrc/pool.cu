@@ -304,6 +304,17 @@ int32_t mkv_rotary_turns(const double* inv_freq, int32_t n, uint64_t* turns)
     return MKV_OK;
 }
 
+// Whether n rows of `wa` 16-bit elements, `sa` apart, and n rows of `wb`, `sb` apart, have nothing in common (slices of one
+// buffer included).
+static bool rows_apart(const void* a, int64_t sa, int64_t wa, const void* b, int64_t sb, int64_t wb, int64_t n)
+{
+    const int64_t a0 = (int64_t)(reinterpret_cast<uintptr_t>(a) >> 1), b0 = (int64_t)(reinterpret_cast<uintptr_t>(b) >> 1);
+    if (a0 + (n - 1) * sa + wa <= b0 || b0 + (n - 1) * sb + wb <= a0) return true;
+    if (n == 1 || sa != sb) return false;
+    const int64_t at = ((b0 - a0) % sa + sa) % sa;               // of b's rows behind a's
+    return at >= wa && at + wb <= sa;
+}
+
 int32_t mkv_append_rotary(mkv_pool* pool, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                           int64_t v_stride, const int32_t* slots, const int32_t* positions, int32_t n, const mkv_rotary* r,
                           void* q_out, int64_t out_stride, void* stream)
@@ -321,6 +332,9 @@ int32_t mkv_append_rotary(mkv_pool* pool, const void* q, int64_t q_stride, const
               !aligned(slots, 4)))
         return MKV_E_INVALID;
     if (!aligned(positions, 4)) return MKV_E_INVALID;
+    if (q && !(q == q_out && q_stride == out_stride) && !rows_apart(q_out, out_stride, row_q, q, q_stride, row_q, n)) return MKV_E_INVALID;
+    if (q && k && (!rows_apart(q_out, out_stride, row_q, k, k_stride, row_kv, n) || !rows_apart(q_out, out_stride, row_q, v, v_stride, row_kv, n)))
+        return MKV_E_INVALID;
     return launch_append_rotary(pool, q, q_stride, k, k_stride, v, v_stride, slots, positions, n, r, q_out, out_stride,
                                 (cudaStream_t)stream);
 }
@@ -470,7 +484,8 @@ int32_t mkv_chunk_attention(mkv_pool* pool, const void* q, int64_t q_stride, int
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(ws, 256) || !aligned(bt, 4) || !aligned(lens, 4) || !aligned(starts, 4) ||
         !aligned(lse, 4))
         return MKV_E_INVALID;
-    if (q_stride < (int64_t)pool->hq * pool->d || q_stride % 8) return MKV_E_INVALID;
+    const int64_t row = (int64_t)pool->hq * pool->d;
+    if (q_stride < row || q_stride % 8 || !rows_apart(out, row, row, q, q_stride, row, n_rows)) return MKV_E_INVALID;
     if (!(scale - scale == 0.f)) return MKV_E_INVALID;              // infinite, or not a number
     if (ws_bytes < chunk_ws_bytes(pool->d, B, max_pages)) return MKV_E_INVALID;
     return launch_chunk_attention(pool, q, q_stride, n_rows, starts, bt, tags, lens, B, max_pages, scale, out, lse, ws,

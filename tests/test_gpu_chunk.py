@@ -406,12 +406,17 @@ def test_refusals_on_a_device_pool():
                 dict(seq_lens=lens.cpu()), dict(q=q[..., ::2].repeat(1, 1, 2)[..., ::2])):
         with pytest.raises((AssertionError, M.MkvError)):
             pool.chunk_attention(**{**ok, **bad})
-    for bad in (dict(scale=float("nan")), dict(scale=float("inf")), dict(workspace=ws[:1024])):
+    same = torch.zeros(2 * q.numel(), dtype=torch.bfloat16, device="cuda")
+    for bad in (dict(scale=float("nan")), dict(scale=float("inf")), dict(workspace=ws[:1024]), dict(out=q),
+                dict(q=same[:q.numel()].view(q.shape), out=same[512:512 + q.numel()].view(q.shape))):
         with pytest.raises(M.MkvError) as e:
             pool.chunk_attention(**{**ok, **bad})
         assert e.value.code == M.E_INVALID
     torch.cuda.synchronize()
-    assert (out == 2).all() and pool.status() == M.OK
+    assert (out == 2).all() and not same.any() and pool.status() == M.OK
+    # a row of its own has no stride to speak of
+    one = pool.chunk_attention(q[3:].as_strided((1, 4, 128), (8, 128, 1)), torch.tensor([0, 1], dtype=torch.int32, device="cuda"), table, tags, lens, 0.1)
+    assert torch.equal(one[0], pool.chunk_attention(q, starts, table, tags, lens, 0.1)[3]) and pool.status() == M.OK
     empty = pool.chunk_attention(q[:0], torch.zeros(2, dtype=torch.int32, device="cuda"), table, tags, lens, 0.1)
     assert empty.shape == (0, 4, 128)
 

@@ -205,6 +205,29 @@ def test_refusals_on_a_device_pool():
 
 
 @gpu
+def test_outputs_that_overlap_inputs_are_refused_and_slices_of_one_buffer_are_not():
+    n, hq, hkv, d = 5, 4, 2, 128
+    pool, other = (M.Pool(d, hkv, hq, 4, 1, np.ones(d, np.int8)) for _ in range(2))
+    rot = M.Rotary(frequencies(64))
+    wide = torch.zeros(n, hq + 2 * hkv + hq + 1, d, dtype=torch.bfloat16, device="cuda")
+    wide[:, :hq + 2 * hkv] = torch.randn(n, hq + 2 * hkv, d, device="cuda").bfloat16()
+    before = wide.clone()
+    q, k, v, room = wide.split([hq, hkv, hkv, hq + 1], 1)
+    slots, pos = (torch.arange(n, dtype=torch.int32, device="cuda") for _ in range(2))
+    flat = wide.view(-1)
+    for bad in (wide[:, 1:1 + hq], wide[:, 5:5 + hq], flat[:n * hq * d].view(n, hq, d), flat[d:d + n * hq * d].view(n, hq, d)):
+        with pytest.raises(M.MkvError) as e:
+            pool.append_rotary(q, k, v, slots, pos, rot, q_out=bad)
+        assert e.value.code == M.E_INVALID
+    torch.cuda.synchronize()
+    assert torch.equal(wide, before) and not pool.fp8_arena.any()
+    want = other.append_rotary(q, k, v, slots, pos, rot)
+    pool.append_rotary(q, k, v, slots, pos, rot, q_out=room[:, 1:])
+    assert torch.equal(room[:, 1:], want) and torch.equal(wide[:, :hq + 2 * hkv], before[:, :hq + 2 * hkv])
+    assert torch.equal(pool.fp8_arena, other.fp8_arena)
+
+
+@gpu
 @pytest.mark.parametrize("d,hkv,group,fmt", [(256, 2, 6, 2), (128, 2, 4, 1)])
 def test_prompt_demotion_and_drafts_as_a_server_runs_them(d, hkv, group, fmt):
     """A prompt in chunks (rotated Append, chunk attention), its old pages demoted, then draft tokens and a decode step: every
