@@ -1,10 +1,21 @@
 """Refusals of mkv_chunk_attention that need no device: nothing is launched."""
 import ctypes as C
+import os
+import re
 
 import numpy as np
 import pytest
 
 import paper_2608_23834_b200 as M
+from conftest import ROOT
+
+
+@pytest.mark.parametrize("name", ["chunk_attention.cu", "tensor_ptx.cuh"])
+def test_no_read_only_loads_in_kernels_that_start_early(name):
+    """The plan, scan and merge kernels start while their predecessors still write (as in test_early_launch_loads)."""
+    with open(os.path.join(ROOT, "paper_2608_23834_b200", "csrc", name)) as f:
+        code = re.sub(r"//[^\n]*|/\*.*?\*/", "", f.read(), flags=re.S)
+    assert not re.findall(r"__ldg\b|ld\.global\.nc|\bconst\s+\w+\s*\*\s*__restrict__", code)
 
 
 def test_workspace_grows_with_the_table_and_bad_sizes_are_refused():
