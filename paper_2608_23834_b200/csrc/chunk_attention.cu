@@ -27,16 +27,16 @@
 //     (m, l, O) in the workspace and chunk_merge_kernel joins them (Eq. softmax-merge), in the order of the blocks.
 //
 // What bounds it (B200; measured with the arenas in HBM, rates are of the visible pairs' 4 d flops):
-//   * Long chunks, d = 256 (2,048 rows of 24 heads over 57K tokens, format 2): 2.9 ms, 1.0 PFLOP/s, 60 % of what a large bf16
-//     matrix product reaches here.  The data path of shared memory is 80 % busy: unpacked tiles are stored and then read by
+//   * Long chunks, d = 256 (2,048 rows of 24 heads over 57K tokens, format 2): 2.9 to 3.1 ms by the clock that the power cap leaves,
+//     0.95 - 1.0 PFLOP/s, 57 - 60 % of what a large bf16 matrix product reaches here.  The data path of shared memory is 80 % busy: unpacked tiles are stored and then read by
 //     the products of one row tile; unpacking left out, it would be 2.3 ms.  Sharing a tile between two SMs would halve that.
-//   * d = 128 (1,000 rows of 32 heads over 16K tokens, twice): 0.8 ms, 0.69 PFLOP/s.  The softmax: 128 columns take a warp 2,000
+//   * d = 128 (1,000 rows of 32 heads over 16K tokens, twice): 0.78 ms, 0.71 PFLOP/s.  The softmax: 128 columns take a warp 2,000
 //     cycles alone, 3,200 with a second one on its scheduler, 4,600 with two unpacking warps besides.  Score buffers of 64 columns,
 //     four of them, hide the wait for the scores and lose more in steps (0.9 ms); two threads to a row, the softmax fully unrolled,
 //     wider tensor-memory loads (registers) and unpacking split by keys and values were slower, too.
-//   * Prompts (3 x 4,097 rows, d = 256): 0.75 ms, half of the rate: the causal half of the last tiles is masked, and a unit's query
-//     and epilogue cost as much as six key tiles.
-//   * A few rows per request: latency.  4 rows over 4,092 tokens: 29 us in three launches, of which the plan takes 4, the scan's start
+//   * Prompts (3 x 4,097 rows, d = 256): 0.70 ms, half of the rate: the causal half of the last tiles is masked, and a unit's query
+//     and epilogue cost as much as four to five key tiles (0.74 ms with six of them in the cut and one price for all tiles, 0.89 with two).
+//   * A few rows per request: latency.  4 rows over 4,092 tokens: 30 us in three launches, of which the plan takes 4, the scan's start
 //     (share, query, first keys) 6, its two tiles 5, partials and merge 7.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -51,10 +51,10 @@ namespace chunk {
 
 constexpr int kMaxBlocks = 160;              // of the scan's grid: sizes the partials
 constexpr int kKeys = 128;                   // keys of a tile: eight runs of 16 tokens
-// What a unit costs besides its key tiles (query, epilogue), in key tiles: 3 prompts of 4,097 tokens 0.75 ms with 6 and 8, 0.89
-// with 2; 16 mixed requests 0.35 and 0.43.
-constexpr int kUnitCost = 6;
-constexpr int kLeastShare = 2;               // of a block, in key tiles: smaller shares cost more in partials than they save
+// The cut's prices: of a key tile, of one in a unit that fills one of two row tiles, and of a unit besides (query, epilogue).
+// Measured: 3.0, 1.8 and 12 - 20 us at d = 128, 2.25 and 9.5 at d = 256.
+constexpr int kTileCost = 5, kHalfTileCost = 3, kUnitCost = 24;
+constexpr int kLeastShare = 2 * kTileCost;   // of a block: smaller shares cost more in partials than they save
 constexpr float kShift = 7.f, kSlack = 8.f;  // see above: probabilities are at most 2^(kShift + kSlack)
 constexpr int kNoPos = 0x7fffffff;
 
@@ -68,7 +68,7 @@ struct Request {
     int stale_end;               // runs of the row up to the last Stale page
     int exact;                   // every page of the row is in a list
     int pad;
-    long long cost;              // of one KV head: the units' key tiles + kUnitCost each
+    long long cost;              // of one KV head: its units'
 };
 struct Merge {
     int b, h, rt, last;          // unit, last block that has a part of it; b < 0: nothing to merge
@@ -130,6 +130,17 @@ __device__ __forceinline__ Unit unit_of(const Request& r, int group, int rt)
     return u;
 }
 
+template <int ROWS>
+__device__ __forceinline__ int row_tiles_of(const Request& r, int group, int rt) { return min(ROWS / 128, (r.n_new * group - rt * ROWS + 127) / 128); }
+template <int ROWS>
+__device__ __forceinline__ int tile_cost(const Request& r, int group, int rt) { return row_tiles_of<ROWS>(r, group, rt) * 128 == ROWS ? kTileCost : kHalfTileCost; }
+template <int ROWS>
+__device__ __forceinline__ int unit_cost(const Request& r, int group, int rt)
+{
+    const Unit u = unit_of<ROWS>(r, group, rt);
+    return kUnitCost + (u.stale_tiles + u.fp8_tiles) * tile_cost<ROWS>(r, group, rt);
+}
+
 struct Segment {
     Request r;
     Unit u;
@@ -153,13 +164,39 @@ struct Walk {
     long long at;
     int b, h, rt;
 
-    __device__ __forceinline__ void open(const Params& P, const Share* share)
+    // To the unit where the share begins (the whole warp, 32 units at a time).
+    template <int ROWS>
+    __device__ __forceinline__ void open(const Params& P, const Share* share, int lane)
     {
-        b = share->request;
-        rt = 0;
-        const long long cost = P.req[b].cost, skip = (share->p0 - share->request_start) / cost;      // KV heads before the first unit
-        h = (int)skip;
-        at = share->request_start + skip * cost;
+        const Request r = P.req[share->request];
+        const long long skip = (share->p0 - share->request_start) / r.cost;      // KV heads before the first unit
+        const int n_rt = (r.n_new * P.group + ROWS - 1) / ROWS;
+        long long pos = share->request_start + skip * r.cost;
+        int first = 0;
+        for (; first < n_rt; first += 32) {
+            const int c = first + lane < n_rt ? unit_cost<ROWS>(r, P.group, first + lane) : 0;
+            long long sum = c;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long a = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += a;
+            }
+            const uint32_t m = __ballot_sync(0xffffffffu, pos + sum > share->p0);
+            if (m) {
+                const int src = __ffs(m) - 1;
+                first += src;
+                pos += __shfl_sync(0xffffffffu, sum - c, src);
+                break;
+            }
+            pos += __shfl_sync(0xffffffffu, sum, 31);
+        }
+        if (lane == 0) {
+            b = share->request;
+            h = (int)skip;
+            rt = first;
+            at = pos;
+        }
+        __syncwarp();
     }
     template <int ROWS>
     __device__ __forceinline__ bool next(const Params& P, const Share* share)
@@ -176,8 +213,9 @@ struct Walk {
             const int n = s.u.stale_tiles + s.u.fp8_tiles;
             const long long start = at, first = at + kUnitCost;
             s.b = b; s.h = h; s.rt = rt;
-            s.nt = min(ROWS / 128, (s.r.n_new * P.group - rt * ROWS + 127) / 128);
-            at = first + n;
+            s.nt = row_tiles_of<ROWS>(s.r, P.group, rt);
+            const int price = tile_cost<ROWS>(s.r, P.group, rt), all = n * price;
+            at = first + all;
             if (++rt == n_rt) {
                 rt = 0;
                 if (++h == P.hkv) {
@@ -185,14 +223,14 @@ struct Walk {
                     ++b;
                 }
             }
-            s.t0 = (int)max(0ll, p0 - first);
-            s.t1 = (int)min((long long)n, p1 - first);
-            if (n == 0) s.t0 = s.t1 = 0;                         // rows that see nothing
+            // a tile is the block's in whose share it begins (a share is longer than any tile)
+            s.t0 = ((int)min((long long)all, max(0ll, p0 - first)) + price - 1) / price;
+            s.t1 = ((int)min((long long)all, max(0ll, p1 - first)) + price - 1) / price;
             if (s.t1 > s.t0 || (n == 0 && start >= p0)) {
                 const bool whole = s.t0 == 0 && s.t1 == n;
                 s.slot = whole ? -1 : 2 * (int)blockIdx.x + (start >= p0 ? 1 : 0);
                 s.first_part = !whole && s.t0 == 0;
-                s.last_block = (int)((first + n - 1) / share->per);
+                s.last_block = n > 0 ? (int)((first + (n - 1) * price) / share->per) : (int)blockIdx.x;
                 return true;
             }
         }
@@ -314,10 +352,7 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const Params P
     r.stale_end = stale_end_s;
     const int n_rt = (n_new * P.group + ROWS - 1) / ROWS;
     long long cost = 0;
-    for (int rt = tid; rt < n_rt; rt += kPlanThreads) {
-        const Unit u = unit_of<ROWS>(r, P.group, rt);
-        cost += u.stale_tiles + u.fp8_tiles + kUnitCost;
-    }
+    for (int rt = tid; rt < n_rt; rt += kPlanThreads) cost += unit_cost<ROWS>(r, P.group, rt);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) cost += __shfl_xor_sync(0xffffffffu, cost, o);
     if (lane == 0 && cost) atomicAdd(reinterpret_cast<unsigned long long*>(&cost_s), (unsigned long long)cost);
@@ -596,8 +631,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
     constexpr uint32_t kColS = NT * D;                           // O: NT x D columns, then two score buffers
     Walk* walk = reinterpret_cast<Walk*>(smem + G::OFF_WALK) + warp;
     const Segment& s = walk->s;
-    if (lane == 0) walk->open(P, share);
-    __syncwarp();
+    walk->open<ROWS>(P, share, lane);
     auto next_segment = [&]() -> bool {
         __syncwarp();                                            // the segment before is no longer looked at
         bool more = false;
