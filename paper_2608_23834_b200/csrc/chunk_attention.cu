@@ -21,8 +21,8 @@
 //   * One warp issues the products S = Q K^T (both operands in shared memory) and O += P V (P in tensor memory, over
 //     the scores it came from), the scores of the tile after next before the softmax of this one has finished.
 //   * A softmax thread owns a row (its tensor-memory lane): no exchange between threads.  The reference of the
-//     exponentials is raised only when a score exceeds it by 2^15, which keeps P within fp16 and rescaling of O rare;
-//     it lies 7 below the maximum, so that probabilities down to 2^-31 of the largest are not flushed.
+//     exponentials is raised only when 32 of them sum to more than 2^15, which keeps P within fp16 and rescaling of O rare;
+//     it is set 7 below the maximum, so that probabilities down to 2^-31 of the largest are not flushed.
 //   * (unit, key tiles) pairs are cut evenly over the SMs; a unit that several blocks share leaves fp32 partials
 //     (m, l, O) in the workspace and chunk_merge_kernel joins them (Eq. softmax-merge), in the order of the blocks.
 //
@@ -55,7 +55,8 @@ constexpr int kKeys = 128;                   // keys of a tile: eight runs of 16
 // Measured: 3.0, 1.8 and 12 - 20 us at d = 128, 2.25 and 9.5 at d = 256.
 constexpr int kTileCost = 5, kHalfTileCost = 3, kUnitCost = 24;
 constexpr int kLeastShare = 2 * kTileCost;   // of a block: smaller shares cost more in partials than they save
-constexpr float kShift = 7.f, kSlack = 8.f;  // see above: probabilities are at most 2^(kShift + kSlack)
+constexpr float kShift = 7.f;                // see above: the reference lies so far below the maximum when it is set
+constexpr float kMostSum = 32768.f;          // of the probabilities of a step, so of any of them: fp16 holds them
 constexpr int kNoPos = 0x7fffffff;
 
 template <int N>
@@ -249,7 +250,7 @@ struct Geo {
     static constexpr int MMA_WARP = SOFT_WARPS + UNPACK_WARPS, THREADS = 32 * (MMA_WARP + 4);
     // registers: of the launch, and of the softmax, unpacking and product warps afterwards (the sums agree)
     static constexpr int REGS = D == 128 ? 96 : 128;
-    static constexpr int SOFT_REGS = D == 128 ? 104 : 128, UNPACK_REGS = D == 128 ? 104 : 152, MMA_REGS = D == 128 ? 64 : 80;
+    static constexpr int SOFT_REGS = D == 128 ? 112 : 128, UNPACK_REGS = D == 128 ? 104 : 152, MMA_REGS = D == 128 ? 48 : 80;
     static_assert(SOFT_WARPS * SOFT_REGS + UNPACK_WARPS * UNPACK_REGS + 4 * MMA_REGS <= (MMA_WARP + 4) * REGS, "register split");
     static constexpr int OFF_Q = 0, OFF_K = OFF_Q + NT * Q_TILE, OFF_V = OFF_K + STAGES * K_TILE;
     static constexpr int OFF_FAC = OFF_V + STAGES * V_TILE;     // factor of every row's scores
@@ -1281,69 +1282,72 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                     }
                     const float2 fac2 = make_float2(fac, fac);
                     if (turn) scale_output(__uint_as_float((uint32_t)(127 + P.ve) << 23) / P.v_scale);
-                    // Exponentials against the reference so far; where a score exceeds it by too much (as a rule only in a
-                    // unit's first tile) it is raised by whole powers of two, and what was summed or stored before is scaled
-                    // down exactly
+                    // Exponentials against the reference so far.  Their sum shows where one has grown too large for fp16 (as a rule
+                    // only in a unit's first tile): the reference is then raised by whole powers of two, what was summed or stored
+                    // before is scaled down exactly, and the columns are taken again.
 #pragma unroll 1
                     for (int c = 0; c < kKeys / COLS; ++c) {
-                        float x[COLS], m4[4];
-                        tmem_ld_n(col_s + COLS * c, x);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) m4[q] = fmaxf(x[q], x[q + 4]);
-#pragma unroll
-                        for (int k = 8; k < COLS; k += 8)
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) m4[q] = fmaxf(m4[q], fmaxf(x[k + q], x[k + q + 4]));
-                        const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * fac;
-                        const bool raise = mx > ref + (kShift + kSlack);
-                        if (__any_sync(FULL, raise)) {
-                            float f = 1.f;
-                            if (raise) {
-                                const float to = ref == -CUDART_INF_F ? mx - kShift : ref + ceilf(mx - kShift - ref);
-                                f = ref == -CUDART_INF_F ? 0.f : exp2f(ref - to);
-                                ref = to;
-                            }
-                            sum *= f;
-                            if (n_done > 0) scale_output(f);
-                            const uint32_t f2 = pack_f16x2(f, f);
-#pragma unroll 1
-                            for (int p = 0; p < c * COLS / 16; ++p) {    // the probabilities of the columns before these
-                                uint32_t y[8];
-                                tmem_ld8_u32(col_s + 8 * p, y);
-                                tmem_wait_ld();
-#pragma unroll
-                                for (int k = 0; k < 8; ++k) y[k] = hmul2_u32(y[k], f2);
-                                tmem_st_n(col_s + 8 * p, y);
-                            }
-                        }
-                        const float base = ref == -CUDART_INF_F ? 0.f : ref;
-                        const float2 base2 = make_float2(-base, -base);
-                        float2 s2[4];
+                        float part;
                         uint32_t h2[COLS / 2];
-                        if constexpr (D == 256) {                // one warp a scheduler: in sweeps, no pair waits for its own steps
+#pragma unroll 1
+                        for (bool again = false;; again = true) {
+                            float x[COLS];
+                            tmem_ld_n(col_s + COLS * c, x);
+                            tmem_wait_ld();
+                            if (again) {
+                                float mx = x[0];
 #pragma unroll
-                            for (int k = 0; k < COLS; k += 2) {
-                                const float2 e = fma2(make_float2(x[k], x[k + 1]), fac2, base2);
-                                x[k] = e.x;
-                                x[k + 1] = e.y;
+                                for (int k = 1; k < COLS; ++k) mx = fmaxf(mx, x[k]);
+                                mx *= fac;
+                                const bool raise = (part > kMostSum || ref == -CUDART_INF_F) && mx > ref + kShift;
+                                float f = 1.f;
+                                if (raise) {
+                                    const float to = ref == -CUDART_INF_F ? mx - kShift : ref + ceilf(mx - kShift - ref);
+                                    f = ref == -CUDART_INF_F ? 0.f : exp2f(ref - to);
+                                    ref = to;
+                                }
+                                sum *= f;
+                                if (n_done > 0) scale_output(f);
+                                const uint32_t f2 = pack_f16x2(f, f);
+#pragma unroll 1
+                                for (int p = 0; p < c * COLS / 16; ++p) {    // the probabilities of the columns before these
+                                    uint32_t y[8];
+                                    tmem_ld8_u32(col_s + 8 * p, y);
+                                    tmem_wait_ld();
+#pragma unroll
+                                    for (int k = 0; k < 8; ++k) y[k] = hmul2_u32(y[k], f2);
+                                    tmem_st_n(col_s + 8 * p, y);
+                                }
+                            }
+                            const float base = ref == -CUDART_INF_F ? 0.f : ref;
+                            const float2 base2 = make_float2(-base, -base);
+                            float2 s2[4];
+                            if constexpr (D == 256) {            // one warp a scheduler: in sweeps, no pair waits for its own steps
+#pragma unroll
+                                for (int k = 0; k < COLS; k += 2) {
+                                    const float2 e = fma2(make_float2(x[k], x[k + 1]), fac2, base2);
+                                    x[k] = e.x;
+                                    x[k + 1] = e.y;
+                                }
+#pragma unroll
+                                for (int k = 0; k < COLS; ++k) x[k] = exp2_in_order(x[k]);
                             }
 #pragma unroll
-                            for (int k = 0; k < COLS; ++k) x[k] = exp2_in_order(x[k]);
-                        }
-#pragma unroll
-                        for (int k = 0; k < COLS / 2; ++k) {
-                            float2 e = make_float2(x[2 * k], x[2 * k + 1]);
-                            if constexpr (D == 128) {
-                                e = fma2(e, fac2, base2);
-                                e.x = fast_exp2(e.x);
-                                e.y = fast_exp2(e.y);
+                            for (int k = 0; k < COLS / 2; ++k) {
+                                float2 e = make_float2(x[2 * k], x[2 * k + 1]);
+                                if constexpr (D == 128) {
+                                    e = fma2(e, fac2, base2);
+                                    e.x = fast_exp2(e.x);
+                                    e.y = fast_exp2(e.y);
+                                }
+                                s2[k & 3] = k < 4 ? e : add2(s2[k & 3], e);
+                                h2[k] = pack_f16x2(e.x, e.y);
                             }
-                            s2[k & 3] = k < 4 ? e : add2(s2[k & 3], e);
-                            h2[k] = pack_f16x2(e.x, e.y);
+                            s2[0] = add2(add2(s2[0], s2[1]), add2(s2[2], s2[3]));
+                            part = s2[0].x + s2[0].y;
+                            if (again || !__any_sync(FULL, part > kMostSum || ref == -CUDART_INF_F)) break;
                         }
-                        s2[0] = add2(add2(s2[0], s2[1]), add2(s2[2], s2[3]));
-                        sum += s2[0].x + s2[0].y;
+                        sum += part;
                         tmem_st_n(col_s + COLS / 2 * c, h2);
                     }
                     tmem_wait_st();
