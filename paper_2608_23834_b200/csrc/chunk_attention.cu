@@ -28,12 +28,14 @@
 //
 // What bounds it (B200; measured with the arenas in HBM, rates are of the visible pairs' 4 d flops):
 //   * Long chunks, d = 256 (2,048 rows of 24 heads over 57K tokens, format 2): 2.9 to 3.1 ms by the clock that the power cap leaves,
-//     0.95 - 1.0 PFLOP/s, 57 - 60 % of what a large bf16 matrix product reaches here.  The data path of shared memory is 80 % busy: unpacked tiles are stored and then read by
-//     the products of one row tile; unpacking left out, it would be 2.3 ms.  Sharing a tile between two SMs would halve that.
-//   * d = 128 (1,000 rows of 32 heads over 16K tokens, twice): 0.78 ms, 0.71 PFLOP/s.  The softmax: 128 columns take a warp 2,000
-//     cycles alone, 3,200 with a second one on its scheduler, 4,600 with two unpacking warps besides.  Score buffers of 64 columns,
-//     four of them, hide the wait for the scores and lose more in steps (0.9 ms); two threads to a row, the softmax fully unrolled,
-//     wider tensor-memory loads (registers) and unpacking split by keys and values were slower, too.
+//     0.95 - 1.0 PFLOP/s, 57 - 60 % of what a large bf16 matrix product reaches here.  The data path of shared memory is 80 % busy:
+//     unpacked tiles are stored and then read by the products of one row tile; unpacking left out, it would be 2.3 ms.  Sharing a
+//     tile between two SMs would halve that.
+//   * d = 128 (1,000 rows of 32 heads over 16K tokens, twice): 0.74 ms, 0.74 PFLOP/s.  The softmax, chains of two warps a scheduler
+//     beside two unpacking ones: a step of 32 columns costs some 240 cycles whatever it does (steps of 16: 0.98 ms; of 64: registers).
+//     Spilled registers count: 104 for a softmax thread 0.85 ms, 112 0.74.  Score buffers of 64 columns, four of them, hide the wait for
+//     the scores and lose more in steps (0.9 ms for 0.8); two threads to a row, the softmax fully unrolled and unpacking split by keys
+//     and values were slower, too.
 //   * Prompts (3 x 4,097 rows, d = 256): 0.70 ms, half of the rate: the causal half of the last tiles is masked, and a unit's query
 //     and epilogue cost as much as four to five key tiles (0.74 ms with six of them in the cut and one price for all tiles, 0.89 with two).
 //   * A few rows per request: latency.  4 rows over 4,092 tokens: 30 us in three launches, of which the plan takes 4, the scan's start
@@ -134,7 +136,10 @@ __device__ __forceinline__ Unit unit_of(const Request& r, int group, int rt)
 template <int ROWS>
 __device__ __forceinline__ int row_tiles_of(const Request& r, int group, int rt) { return min(ROWS / 128, (r.n_new * group - rt * ROWS + 127) / 128); }
 template <int ROWS>
-__device__ __forceinline__ int tile_cost(const Request& r, int group, int rt) { return row_tiles_of<ROWS>(r, group, rt) * 128 == ROWS ? kTileCost : kHalfTileCost; }
+__device__ __forceinline__ int tile_cost(const Request& r, int group, int rt)
+{
+    return row_tiles_of<ROWS>(r, group, rt) * 128 == ROWS ? kTileCost : kHalfTileCost;
+}
 template <int ROWS>
 __device__ __forceinline__ int unit_cost(const Request& r, int group, int rt)
 {
