@@ -96,8 +96,10 @@ class Cache:
         self.dev = [torch.from_numpy(x).cuda() for x in (self.starts, self.table, self.tags, self.lens)]
         return self.dev
 
-    def reference(self, scale=None):
-        """(out, lse, tolerance of out, tolerance of lse) in 64 bits."""
+    def reference(self, scale=None, far=False):
+        """(out, lse, tolerance of out, tolerance of lse) in 64 bits.  far: scores so far apart that two more terms count.  A score
+        is d / 16 additions in fp32, each off by at most 2^-24 of sum |q k|.  A probability below 2^-14 is off by up to 2^-25, half of
+        fp16's least step, where the row's largest is 2^6 at least: 2^-31 of a weight of at most 1."""
         scale = self.scale if scale is None else scale
         n, hq, d = self.q.shape
         out, lse = np.zeros((n, hq, d)), np.full((n, hq), -np.inf)
@@ -121,7 +123,11 @@ class Cache:
                     w /= w.sum()
                     out[r, h] = w @ v
                     e = 1.05 * 2.0 ** -10 * abs(scale) * (kr @ qr[r, h]).max()
+                    if far:
+                        e += self.d / 16 * 2.0 ** -24 * abs(scale) * (np.abs(k) @ np.abs(q[r, h])).max()
                     tol[r, h] = 2.0 ** -8 * np.abs(out[r, h]) + (np.expm1(2 * e) + 2.0 ** -10 + 2.0 ** -13) * (w @ np.abs(v)) + 1e-30
+                    if far:
+                        tol[r, h] += 2.0 ** -31 * np.abs(v).sum(0)
                     tol_lse[r, h] = e + 2.0 ** -16 * (1 + abs(lse[r, h]))
         return out, lse, tol, tol_lse
 
@@ -465,3 +471,30 @@ def test_nan_in_several_units_of_a_block(d, group):
         assert pool.status() == M.OK and torch.equal(out.isnan().cpu(), want) and lse.isfinite().all()
     ref = c.reference()
     c.check(torch.where(want.cuda(), torch.from_numpy(ref[0]).cuda().bfloat16(), out), lse, ref)
+
+
+@gpu
+@pytest.mark.parametrize("d,group", [(128, 8), (128, 3), (256, 5)])
+@pytest.mark.parametrize("scale", [1.5, -0.6])
+def test_scores_that_keep_rising_and_falling(d, group, scale):
+    """Scores hundreds of nats apart: every row's reference is raised many times, what lies far below it vanishes."""
+    c = Cache(d, 1, group, [(900, 5), (300, 300), (2600, 2), (40, 40)], 1, seed=81, stale=0.0)
+    ramp = lambda n: np.float32(2.0) ** np.round(np.linspace(-6, 3, n))[:, None]
+    for b, up in enumerate((True, False, True, True)):
+        n = int(c.lens[b])
+        factor = ramp(n) if up else ramp(n)[::-1]                      # powers of two: e4m3 holds the products or their rounding
+        for p in range(-(-n // 16)):
+            at, m = 16 * p, min(16, n - 16 * p)
+            k = np.zeros((16, d), np.float32)
+            k[:m] = c.k[b][at:at + m, 0] * factor[at:at + m]
+            v = np.zeros((16, d), np.float32)
+            v[:m] = c.v[b][at:at + m, 0]
+            rec = oracle.fp8_pack_block(k, v, m, 1.0, 1.0)
+            c.fp8[c.table[b, p], 0] = rec
+            kf, vf = oracle.fp8_unpack_block_f32(rec, d, 1, 1.0, 1.0)
+            c.k[b][at:at + m, 0], c.v[b][at:at + m, 0] = kf[:m], vf[:m]
+    out, lse, pool = run(c, scale=scale)
+    assert pool.status() == M.OK
+    ref = c.reference(scale, far=True)
+    assert np.ptp(ref[1][np.isfinite(ref[1])]) > 100
+    c.check(out, lse, ref)
