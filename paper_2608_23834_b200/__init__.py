@@ -7,6 +7,7 @@ exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Optional
@@ -174,6 +175,19 @@ def _stream(stream: Optional[torch.cuda.Stream]):
     return C.c_void_p(s.cuda_stream)
 
 
+@contextlib.contextmanager
+def _launching_on(stream: Optional[torch.cuda.Stream], device: torch.device):
+    """The pool's device and the stream that the kernels run on are the current ones: what is allocated or filled in between
+    comes before the kernels and is not handed out again before they have passed."""
+    if stream is None:
+        with torch.cuda.device(device):
+            yield
+    else:
+        assert stream.device == device, "stream: one of the pool's device"
+        with torch.cuda.stream(stream):
+            yield
+
+
 def make_config(head_dim, n_kv_heads, n_q_heads, fp8_pages, tq3_pages, sigma: np.ndarray, k_scale=1.0, v_scale=1.0,
                 page_tokens=16, tq3_format=1):
     sig = np.ascontiguousarray(sigma, dtype=np.int8)
@@ -332,14 +346,14 @@ class Pool:
                                                                   rotary.turns, rotary.n_axes, q_out, stream), "mkv_append_rotary"):
             return q_out
         assert (k is None) == (v is None) and (q is not None or k is not None), "q, or k and v, or all"
-        n = (q if q is not None else k).shape[0]
+        n, ours = (q if q is not None else k).shape[0], q is not None and q_out is None
         tensors = [positions, rotary.turns]
         if q is not None:
             self._check_rows(q, n, self.hq, "q")
-            if q_out is None:
-                q_out = torch.empty((n, self.hq, self.d), dtype=torch.bfloat16, device=q.device)
-            self._check_rows(q_out, n, self.hq, "q_out")
-            tensors += [q, q_out]
+            if not ours:
+                self._check_rows(q_out, n, self.hq, "q_out")
+                tensors.append(q_out)
+            tensors.append(q)
         else:
             assert q_out is None, "q_out without q"
         if k is not None:
@@ -352,10 +366,14 @@ class Pool:
         assert rotary.rotary_dim <= self.d, "rotary_dim: at most head_dim"
         assert all(t.device == self.fp8_arena.device for t in tensors), "every tensor is on the pool's device"
         step = lambda t, heads: 0 if t is None else t.stride(0) if n > 1 else heads * self.d
-        with torch.cuda.device(self.fp8_arena.device):
+        with _launching_on(stream, self.fp8_arena.device):
+            if ours:
+                q_out = torch.empty((n, self.hq, self.d), dtype=torch.bfloat16, device=q.device)
             _check(lib().mkv_append_rotary(self.handle, _ptr(q), step(q, self.hq), _ptr(k), step(k, self.hkv), _ptr(v), step(v, self.hkv),
                                            _ptr(slot_mapping) if k is not None else None, _ptr(positions), n, C.byref(rotary.struct),
                                            _ptr(q_out), step(q_out, self.hq), _stream(stream)), "mkv_append_rotary")
+        if ours:
+            self._handed_over(q_out, stream)
         return q_out
 
     def demote(self, src_ids: torch.Tensor, dst_ids: torch.Tensor, block_table=None, tier_tag=None, entry_index=None,
@@ -449,21 +467,31 @@ class Pool:
         assert block_table.dtype == torch.int32 and block_table.is_contiguous() and block_table.dim() == 2 and block_table.shape[0] == B
         assert tier_tag.dtype == torch.uint8 and tier_tag.is_contiguous() and tier_tag.shape == block_table.shape
         assert seq_lens.dtype == torch.int32 and seq_lens.is_contiguous()
-        if out is None:
-            out = torch.zeros((n, self.hq, self.d), dtype=torch.bfloat16, device=q.device)
-        assert out.dtype == torch.bfloat16 and out.is_contiguous() and out.shape == q.shape
+        ours = out is None
+        if not ours:
+            assert out.dtype == torch.bfloat16 and out.is_contiguous() and out.shape == q.shape
         if lse is not None:
             assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2]
-        if workspace is None:
-            workspace = self.chunk_workspace(max(B, 1), max(block_table.shape[1], 1))
-        assert workspace.dtype == torch.uint8 and workspace.is_contiguous()
-        tensors = [q, q_starts, block_table, tier_tag, seq_lens, out, workspace] + ([lse] if lse is not None else [])
+        if workspace is not None:
+            assert workspace.dtype == torch.uint8 and workspace.is_contiguous()
+        tensors = [t for t in (q, q_starts, block_table, tier_tag, seq_lens, out, lse, workspace) if t is not None]
         assert all(t.device == self.fp8_arena.device for t in tensors), "every tensor is on the pool's device"
-        with torch.cuda.device(self.fp8_arena.device):
+        with _launching_on(stream, self.fp8_arena.device):
+            if ours:
+                out = torch.zeros((n, self.hq, self.d), dtype=torch.bfloat16, device=q.device)
+            if workspace is None:
+                workspace = self.chunk_workspace(max(B, 1), max(block_table.shape[1], 1))
             _check(lib().mkv_chunk_attention(self.handle, _ptr(q), q.stride(0) if n > 1 else self.hq * self.d, n, _ptr(q_starts), _ptr(block_table), _ptr(tier_tag),
                                              _ptr(seq_lens), B, block_table.shape[1], float(scale), _ptr(out), _ptr(lse),
                                              _ptr(workspace), workspace.numel(), _stream(stream)), "mkv_chunk_attention")
+        if ours:
+            self._handed_over(out, stream)
         return out
+
+    def _handed_over(self, out, stream):
+        """`out` was allocated on `stream`, for a caller on the current one, who may drop it while its own kernels read it."""
+        if stream is not None and out.is_cuda:
+            out.record_stream(torch.cuda.current_stream(out.device))
 
     def _check_rows(self, x, n, heads, name):
         """bf16 [n][heads][d] whose tokens may lie apart: heads and dims dense, tokens a multiple of 16 bytes apart."""
