@@ -1221,6 +1221,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                     for (int k = 0; k < 8; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * f);
                     tmem_st_n(col_o + 8 * c, y);
                 }
+                tmem_wait_st();                                  // (it may be scaled again in the same tile)
             };
             ++segments;
             // one row tile where there is room for two: both groups take its rows, and the key tiles by turns
@@ -1300,6 +1301,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                             tmem_ld_n(col_s + COLS * c, x);
                             tmem_wait_ld();
                             if (again) {
+                                tmem_wait_st();                  // the probabilities of the columns before these are read again
                                 float mx = x[0];
 #pragma unroll
                                 for (int k = 1; k < COLS; ++k) mx = fmaxf(mx, x[k]);
