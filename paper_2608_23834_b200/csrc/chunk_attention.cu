@@ -569,7 +569,9 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
     unsigned long long* nan_s = reinterpret_cast<unsigned long long*>(smem + G::OFF_NAN);
     const uint32_t failed_at = sb + G::OFF_MISC;                 // word: a wait has given up
     uint32_t* tmem_s = reinterpret_cast<uint32_t*>(smem + G::OFF_MISC + 4);
-    const uint32_t finished_at = sb + G::OFF_MISC + 12;          // word: segments that the softmax warps are done with, summed
+    constexpr int kFinished = 16 + (int)sizeof(Share);           // word per softmax warp: the last segment that it is done with
+    static_assert(kFinished % 4 == 0 && kFinished + 4 * G::SOFT_WARPS <= 128, "words behind the share");
+    const uint32_t finished_at = sb + G::OFF_MISC + kFinished;
     volatile uint32_t* noted_s = reinterpret_cast<volatile uint32_t*>(smem + G::OFF_MISC + 8);    // segment of the latest note
     Share* share = reinterpret_cast<Share*>(smem + G::OFF_MISC + 16);
     // (the warp's number as a uniform value: whole-warp branches are then known as such)
@@ -586,7 +588,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
         }
         sts32(failed_at, 0);
         *noted_s = 0;
-        sts32(finished_at, 0);
+        for (int w = 0; w < G::SOFT_WARPS; ++w) sts32(finished_at + 4 * w, 0);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     for (int i = tid; i < D; i += G::THREADS) nan_s[i] = 0;
@@ -861,10 +863,17 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
             // its bytes are cleared and the channel's first such position is noted; the epilogue gives NaN to the rows
             // from there on.  The note carries the segment, and the epilogue of the segment before is waited for.
             auto note_nan = [&](uint4 (&x)[16 * D / 512], int pos) {
-                // (a count, not a barrier: the roles may be several segments apart)
+                // (Words, not a barrier: the roles may be several segments apart.  One of each warp, not their sum: warps without
+                // rows are done with a segment at once, and with one or two key tiles also with the next.)
+                auto finished = [&] {
+                    bool all = true;
+#pragma unroll
+                    for (int k = 0; k < G::SOFT_WARPS; ++k) all &= lds32(finished_at + 4 * k) + 1 >= segments;
+                    return all;
+                };
                 unsigned long long t0, t1;
                 asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
-                while (lds32(finished_at) < (segments - 1) * G::SOFT_WARPS && !lds32(failed_at)) {
+                while (!finished() && !lds32(failed_at)) {
                     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));
                     if (t1 - t0 > P.wait_ns) {
                         sts32(failed_at, 1);
@@ -1459,7 +1468,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
             }
             __threadfence_block();
             __syncwarp();
-            if (lane == 0) atomicAdd(reinterpret_cast<uint32_t*>(smem + G::OFF_MISC + 12), 1u);
+            if (lane == 0) sts32(finished_at + 4 * warp, segments);
         }
     }
     __syncthreads();
