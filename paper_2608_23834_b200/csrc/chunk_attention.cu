@@ -1299,7 +1299,8 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                     if (turn) scale_output(__uint_as_float((uint32_t)(127 + P.ve) << 23) / P.v_scale);
                     // Exponentials against the reference so far.  Their sum shows where one has grown too large for fp16 (as a rule
                     // only in a unit's first tile): the reference is then raised by whole powers of two, what was summed or stored
-                    // before is scaled down exactly, and the columns are taken again.
+                    // before is scaled down, and the columns are taken again.  (Exactly, but for probabilities that leave fp16's normal
+                    // numbers: 2^-25 or less each time, where the row's largest is 2^6 or more.)
 #pragma unroll 1
                     for (int c = 0; c < kKeys / COLS; ++c) {
                         float part;
@@ -1316,22 +1317,24 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                                 for (int k = 1; k < COLS; ++k) mx = fmaxf(mx, x[k]);
                                 mx *= fac;
                                 const bool raise = (part > kMostSum || ref == -CUDART_INF_F) && mx > ref + kShift;
-                                float f = 1.f;
+                                float up = 0.f;                  // octaves
                                 if (raise) {
-                                    const float to = ref == -CUDART_INF_F ? mx - kShift : ref + ceilf(mx - kShift - ref);
-                                    f = ref == -CUDART_INF_F ? 0.f : exp2f(ref - to);
-                                    ref = to;
+                                    up = ceilf(mx - kShift - ref);               // infinite where there was none
+                                    ref = ref == -CUDART_INF_F ? mx - kShift : ref + up;
                                 }
+                                const float f = exp2f(-up);
                                 sum *= f;
                                 if (n_done > 0) scale_output(f);
-                                const uint32_t f2 = pack_f16x2(f, f);
 #pragma unroll 1
                                 for (int p = 0; p < c * COLS / 16; ++p) {    // the probabilities of the columns before these
                                     uint32_t y[8];
                                     tmem_ld8_u32(col_s + 8 * p, y);
                                     tmem_wait_ld();
 #pragma unroll
-                                    for (int k = 0; k < 8; ++k) y[k] = hmul2_u32(y[k], f2);
+                                    for (int k = 0; k < 8; ++k) {            // (by an fp32 factor: fp16 has no 2^-25, but 2^15 times that)
+                                        const float2 e = half2_to_float2(y[k]);
+                                        y[k] = pack_f16x2(e.x * f, e.y * f);
+                                    }
                                     tmem_st_n(col_s + 8 * p, y);
                                 }
                             }

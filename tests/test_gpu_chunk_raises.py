@@ -82,3 +82,26 @@ def test_a_raise_in_the_tile_that_changes_the_format(d, hkv, group, fmt, v_scale
     out, lse, pool = run(c, scale=scale)
     assert pool.status() == 0
     c.check(out, lse, c.reference(scale, far=True))
+
+
+@gpu
+@pytest.mark.parametrize("d,hkv,group", [(128, 1, 8), (128, 2, 2), (256, 1, 6), (256, 2, 1)])
+@pytest.mark.parametrize("rise", [14, 24, 26, 28, 30])
+def test_a_raise_by_many_octaves_keeps_what_the_reference_lagged_behind(d, hkv, group, rise):
+    """A probability of 2^14 against the reference (seven octaves above it no raise is due) is 2^(14 - rise) after a raise, which
+    fp16 holds also where it does not hold 2^-rise."""
+    c = Cache(d, hkv, group, [(160, 4), (420, 9)], 1, seed=93, stale=0.0)
+    rng = np.random.RandomState(7)
+    pattern = rng.randint(0, 2, d) * 2.0 - 1
+    set_queries(c, pattern)
+    for b, first in ((0, 0), (1, 128)):                              # in a unit's first key tile, and in a later one
+        n = int(c.lens[b])
+        levels, values = np.zeros(n), rng.randn(n, d).astype(np.float32)
+        levels[first + 40], levels[first + 64:] = 7, rise
+        values[:, 1::2] = 0
+        values[first + 40, 1::2] = 448
+        set_fp8(c, b, levels, values, pattern)
+    scale = octaves(c, 1)
+    out, lse, pool = run(c, scale=scale)
+    assert pool.status() == 0
+    c.check(out, lse, c.reference(scale, far=True))
