@@ -117,6 +117,9 @@ enum {
 // ---- the units --------------------------------------------------------------------------------------
 struct Unit { int stale_tiles, fp8_tiles, n_fp8; };
 
+// (of any length up to 2^31 - 1)
+__device__ __forceinline__ int runs_of(int len) { return ((len - 1) >> 4) + 1; }
+
 // key tiles of the rows [rt * ROWS, (rt + 1) * ROWS) of a request
 template <int ROWS>
 __device__ __forceinline__ Unit unit_of(const Request& r, int group, int rt)
@@ -125,7 +128,7 @@ __device__ __forceinline__ Unit unit_of(const Request& r, int group, int rt)
     const int p = r.len - r.n_new + last;                       // the last position that a row sees
     Unit u = {0, 0, 0};
     if (p < 0) return u;
-    const int run = p >> 4, runs = (r.len + 15) >> 4;
+    const int run = p >> 4, runs = runs_of(r.len);
     // FP8 runs behind the last row's position are left out where they are the row's last runs; elsewhere the masks do it
     u.n_fp8 = r.exact && r.stale_end <= run + 1 ? r.n_fp8 - (runs - 1 - run) : r.n_fp8;
     u.stale_tiles = (r.n_stale + 7) >> 3;
@@ -290,7 +293,7 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const Params P
     if (len < 0) len = 0;
     int n_new = last - first;
     if (first < 0 || last > P.n_rows || n_new < 0) { flags = kStBounds; n_new = 0; }
-    const int pages = n_new > 0 ? (len + T - 1) / T : 0;
+    const int pages = n_new > 0 && len > 0 ? (len - 1) / T + 1 : 0;
     const int32_t* ids = P.bt + (size_t)b * P.max_pages;
     const uint8_t* tags = P.tags + (size_t)b * P.max_pages;
     int2* list = P.list + (size_t)b * P.max_pages;
@@ -1241,7 +1244,7 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
             const int qpos = s.r.len - s.r.n_new + tok;
             const int first_pos = s.r.len - s.r.n_new + (s.rt * ROWS + (by_turns ? 0 : t * 128)) / P.group;
             const int2* list = P.list + (size_t)s.b * P.max_pages;
-            const int cut = s.u.stale_tiles, runs = (s.r.len + 15) >> 4;
+            const int cut = s.u.stale_tiles, runs = runs_of(s.r.len);
             const bool ordinary = s.r.exact && s.r.stale_end * kPage <= first_pos + 1;     // every Stale page lies before the first row
             float ref = -CUDART_INF_F, sum = 0.f, fac = 0.f;
             int n_done = 0;                                      // key tiles of this segment so far
