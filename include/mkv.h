@@ -158,10 +158,11 @@ int32_t mkv_pool_status(mkv_pool* pool, void* stream);
 int32_t mkv_pool_set_decode_variant(mkv_pool* pool, int32_t variant);
 
 /* Wall-time limit, in nanoseconds, of the decode scan's waits for a page copy (Section 4.1: the direct
- * path "fails closed").  Default 20,000,000 (20 ms).  A wait that runs out makes the block stop scanning,
- * wait (with the default limit) for the copies it still has in flight, and finish; the call's output is
- * then not valid and mkv_pool_status() returns MKV_E_TIMEOUT.  0 makes every wait that is not satisfied
- * at once give up: a diagnostic setting that exercises this path. */
+ * path "fails closed"), and of the chunk scan's waits between its warps.  Default 20,000,000 (20 ms).  A
+ * wait that runs out makes the block stop scanning (mkv_chunk_attention: go on without waiting), wait (with
+ * the default limit) for what it still has in flight, and finish; the call's output is then not valid and
+ * mkv_pool_status() returns MKV_E_TIMEOUT.  0 makes every wait that is not satisfied at once give up (of the
+ * chunk scan's, a block's first): a diagnostic setting that exercises this path. */
 int32_t mkv_pool_set_wait_limit_ns(mkv_pool* pool, uint64_t ns);
 
 /* Test hooks: copy one page (all KV heads; n_kv_heads * record bytes) between the arena and a

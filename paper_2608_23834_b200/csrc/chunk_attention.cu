@@ -685,6 +685,11 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                 // job i of the segment: key tile t0 + i / nt, row tile i % nt; its scores are issued two jobs ahead.  With one row
                 // tile where there is room for two, the key tiles go by turns to two accumulators (and softmax groups).
                 const bool by_turns = NT == 2 && nt == 1;
+                // limit 0 (diagnostic): the first look comes while the query's loads are in flight
+                if (P.wait_ns == 0 && fills == 0 && n > 0 && !mbar_test_wait(bar(kQFull), 0)) {
+                    sts32(failed_at, 1);
+                    atomicOr(P.status, kStTimeout);
+                }
                 for (int i = -2; i < n; ++i) {
                     if (i >= 0) {
                         const uint32_t j = nt == 2 ? i >> 1 : i, t = NT == 2 ? i & 1 : 0;
