@@ -358,7 +358,8 @@ int32_t mkv_decode_attention_scored(mkv_pool* pool, const void* q_dev, const int
  * is position p = seq_lens[b] - n_b + i and sees the positions 0 .. p, pages in both formats under one softmax
  * (Section 3.3, Section 4.1).
  *   q            device, bf16 [n_rows][n_q_heads][d], q_stride elements from a token to the next (a multiple of 8, at
- *                least n_q_heads * d: a slice of a fused projection is taken as it stands)
+ *                least n_q_heads * d: a slice of a fused projection is taken as it stands).  A row with an infinity or NaN
+ *                is NaN; so may be one of 2^119 and more, whose rotation overflows
  *   q_starts     device, int32 [B + 1]: first row of every request, ascending from 0 or more; n_b may be 0.  Rows behind
  *                q_starts[B] and before q_starts[0] are neither read nor written.  Rows outside [0, n_rows) or a negative
  *                n_b: the request is left out and the event recorded in the status word

@@ -830,8 +830,8 @@ __global__ void __launch_bounds__(Geo<D>::THREADS, 1) chunk_scan_kernel(const Pa
                         for (int i = 0; i < N; ++i) big = fmaxf(big, fabsf(x[i]));
 #pragma unroll
                         for (int m = 16; m > 0; m >>= 1) big = fmaxf(big, __shfl_xor_sync(FULL, big, m));
-                        int e = (int)(__float_as_uint(big) >> 23) - 126;
-                        if (e < -100 || e > 100) e = 0;                                        // nothing but zeros, or infinities
+                        // (within [1/4, 4) at the ends of fp32's range; zeros and infinities stay what they are)
+                        const int e = min(max((int)(__float_as_uint(big) >> 23) - 126, -126), 126);
                         const float down = __uint_as_float((uint32_t)(127 - e) << 23), up = __uint_as_float((uint32_t)(127 + e) << 23);
                         const float sg = P.negative ? -down : down;
                         uint32_t h2[N / 2];
