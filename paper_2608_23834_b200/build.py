@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import os
+import re
 import subprocess
 import sys
 import sysconfig
@@ -47,6 +48,18 @@ def link_binding(obj):
                     "-l:libmkv.so", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN"], check=True)
 
 
+def check_register_split(log):
+    """The chunk scan's warps share out the registers of its launch (setmaxnreg), so the kernel has to be built with exactly as
+    many as csrc/chunk_attention.cu counts on; a call would be refused otherwise."""
+    with open(os.path.join(CSRC, "chunk_attention.cu")) as f:
+        want = dict(zip(("128", "256"), re.search(r"\bREGS = D == 128 \? (\d+) : (\d+);", f.read()).groups()))
+    # ptxas -v: the entry's name, then (a line of spills between them) what it uses
+    built = re.findall(r"entry function '\w*chunk_scan_kernelILi(\d+)E\w*'(?:(?!entry function).)*?Used (\d+) registers", log, re.S)
+    wrong = [f"head_dim {d}: {n} registers, not {want[d]}" for d, n in built if n != want[d]]
+    if wrong or not built:
+        raise RuntimeError("chunk_scan_kernel: " + ("; ".join(wrong) or "the compiler does not say how many registers it uses"))
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build():
         return LIB
@@ -68,6 +81,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if p.returncode != 0:
             sys.stderr.write(out)
             raise RuntimeError(f"the compiler failed on {src}")
+    check_register_split("\n".join(log))
     subprocess.run([nvcc, "-shared", "-o", LIB, *objs, "-lcudart"], check=True)
     link_binding(binding_obj)
     with open(os.path.join(HERE, "build", "ptxas.log"), "w") as f:
