@@ -15,9 +15,10 @@
 //     take one query: the rotated one for Stale tiles, then the plain one, written over it, for FP8 tiles.
 //   * Pages are unpacked once per block to fp16 in shared memory, K-major with the 128-byte swizzle, by eight warps
 //     (e4m3 -> fp16 is exact; Stale keys are level * g, values code * scale + zero, each rounded to fp16: 2^-12 of an
-//     element on average, as the probabilities' rounding and far below the output's bf16).  A lane of the packed
-//     fragment order holds scattered dims (keys) and tokens (values): the order of the contraction is free, so query dims
-//     and key rows are permuted such that every lane's share is one 16-byte store without bank conflicts.
+//     element on average, as the probabilities' rounding and far below the output's bf16.  The decode kernels, whose output is
+//     fp32, keep such factors apart).  A lane of the packed fragment order holds scattered dims (keys) and tokens (values): the
+//     order of the contraction is free, so query dims and key rows are permuted such that every lane's share is one 16-byte
+//     store without bank conflicts.
 //   * One warp issues the products S = Q K^T (both operands in shared memory) and O += P V (P in tensor memory, over
 //     the scores it came from), the scores of the tile after next before the softmax of this one has finished.
 //   * A softmax thread owns a row (its tensor-memory lane): no exchange between threads.  The reference of the
@@ -26,20 +27,22 @@
 //   * (unit, key tiles) pairs are cut evenly over the SMs; a unit that several blocks share leaves fp32 partials
 //     (m, l, O) in the workspace and chunk_merge_kernel joins them (Eq. softmax-merge), in the order of the blocks.
 //
-// What bounds it (B200; measured with the arenas in HBM, rates are of the visible pairs' 4 d flops):
-//   * Long chunks, d = 256 (2,048 rows of 24 heads over 57K tokens, format 2): 2.9 to 3.1 ms by the clock that the power cap leaves,
-//     0.95 - 1.0 PFLOP/s, 57 - 60 % of what a large bf16 matrix product reaches here.  The data path of shared memory is 80 % busy:
-//     unpacked tiles are stored and then read by the products of one row tile; unpacking left out, it would be 2.3 ms.  Sharing a
-//     tile between two SMs would halve that.
-//   * d = 128 (1,000 rows of 32 heads over 16K tokens, twice): 0.74 ms, 0.74 PFLOP/s.  The softmax, chains of two warps a scheduler
-//     beside two unpacking ones: a step of 32 columns costs some 240 cycles whatever it does (steps of 16: 0.98 ms; of 64: registers).
-//     Spilled registers count: 104 for a softmax thread 0.85 ms, 112 0.74.  Score buffers of 64 columns, four of them, hide the wait for
-//     the scores and lose more in steps (0.9 ms for 0.8); two threads to a row, the softmax fully unrolled and unpacking split by keys
-//     and values were slower, too.
-//   * Prompts (3 x 4,097 rows, d = 256): 0.70 ms, half of the rate: the causal half of the last tiles is masked, and a unit's query
-//     and epilogue cost as much as four to five key tiles (0.74 ms with six of them in the cut and one price for all tiles, 0.89 with two).
-//   * A few rows per request: latency.  4 rows over 4,092 tokens: 30 us in three launches, of which the plan takes 4, the scan's start
-//     (share, query, first keys) 6, its two tiles 5, partials and merge 7.
+// What bounds it (B200; measured with the arenas in HBM, rates are of the visible pairs' 4 d flops): no unit of the SM, but the
+// chains between the roles.
+//   * Long chunks, d = 256 (2,048 rows of 24 heads over 57K tokens, format 2): 3.06 to 3.1 ms by the clock that the power cap leaves,
+//     0.95 PFLOP/s, 57 % of what a large bf16 matrix product reaches here.  On a case of the same kind the tensor pipe is active in 50 % of
+//     the cycles, the data path of shared memory in 53 % (ncu's figure, without the products' operand reads), issue slots in 50 %.  Keys and
+//     values have one stage each: a product waits for two unpacking warps a scheduler, they for it.  Unpacking left out, it would be
+//     2.3 ms; every row tile unpacks every key tile again (96 times a KV head here).
+//   * d = 128 (1,000 rows of 32 heads over 16K tokens, twice): 0.75 ms, 0.73 PFLOP/s; tensor pipe 36 %, issue slots 47 %.  The softmax,
+//     chains of two warps a scheduler beside two unpacking ones: a step of 32 columns costs some 240 cycles whatever it does (steps of 16:
+//     0.98 ms; of 64: registers).  Spilled registers count: 104 for a softmax thread 0.85 ms, 112 0.74 (in one run).  Score buffers of 64
+//     columns, four of them, hide the wait for the scores and lose more in steps (0.9 ms for 0.8); two threads to a row, the softmax fully
+//     unrolled and unpacking split by keys and values were slower, too.
+//   * Prompts (3 x 4,097 rows, d = 256): 0.74 ms, half of the rate: a unit's query, masks and epilogue cost as much as four to five key
+//     tiles, of 17 on average (with six of them in the cut and one price for all tiles 6 % more, with two 27 %).
+//   * A few rows per request: latency.  4 rows over 4,092 tokens: 30 us in three launches: plan 4, the scan's start (share, query, first
+//     keys) 6, then the largest share's key tiles (four, by turns to two accumulators), partials and merge 7, the launches.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math_constants.h>
@@ -56,7 +59,9 @@ constexpr int kKeys = 128;                   // keys of a tile: eight runs of 16
 // The cut's prices: of a key tile, of one in a unit that fills one of two row tiles, and of a unit besides (query, epilogue).
 // Measured: 3.0, 1.8 and 12 - 20 us at d = 128, 2.25 and 9.5 at d = 256.
 constexpr int kTileCost = 5, kHalfTileCost = 3, kUnitCost = 24;
-constexpr int kLeastShare = 2 * kTileCost;   // of a block: smaller shares cost more in partials than they save
+// Of a block: two key tiles, or three to four where a unit fills one of two row tiles; smaller shares cost more in partials than
+// they save.  (Longer than any tile: every block of a unit then begins one.)
+constexpr int kLeastShare = 2 * kTileCost;
 constexpr float kShift = 7.f;                // see above: the reference lies so far below the maximum when it is set
 constexpr float kMostSum = 32768.f;          // of the probabilities of a step, so of any of them: fp16 holds them
 constexpr int kNoPos = 0x7fffffff;
@@ -1558,7 +1563,7 @@ static int32_t launch(const Params& P, int device, int sms, cudaStream_t s)
 {
     using G = Geo<D>;
     // once per device: the kernel's shared memory, and a check that the warps' shares of the registers add up to the launch's (a
-    // build that takes fewer would wait for the rest for ever)
+    // build that takes fewer would wait for the rest for ever; build.py refuses it first)
     static std::mutex mu;
     static unsigned long long ready = 0;                         // a bit per device
     {

@@ -493,7 +493,7 @@ __global__ void __launch_bounds__((kMaxGroup + 1) * D / 16 + D / 2) append_rotar
 // the whole query group.  Keys are written token by token (rows of a record).  Values take the runs that start in the
 // window, as in append_run_kernel: whole tiles leave through shared memory as 16-byte channels.
 // Bound by memory: the key and two query heads are loaded before slots and sines are waited for, and the next two while two
-// are turned.  32,845 tokens of 24 + 4 heads, d = 256 (1.0 GB): 181 us, 85 % of the copy rate; loads where they are needed
+// are turned.  32,845 tokens of 24 + 4 heads, d = 256 (1.0 GB): 181 to 187 us, 83 - 85 % of the copy rate; loads where they are needed
 // 304 us, one head ahead 199, three 204 (spills).  64 registers and 1,024 threads an SM: 181; 80 and 768: 191.
 template <int D, bool INTERLEAVED>
 __global__ void __launch_bounds__(D, 1024 / D) append_rotary_run_kernel(const RotaryArgs A)
